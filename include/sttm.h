@@ -236,6 +236,105 @@ int sttm_positions(sttm_ctx* ctx, const int32_t* cluster_ids_dev, const int32_t*
                    const uint8_t* node_level_dev, const int64_t* offsets_dev, int64_t capacity, int32_t* survived_dev, int32_t* reassigned_dev,
                    float* merged_pos_dev, int32_t* root_tyxl_dev);
 
+/* ---- the reduced sequence in a model: a paged cache of keys and values ---------------------------------------- */
+
+/* The layers behind the merge keep the keys and values of the tokens that are left, answer from them token by token, and
+ * may go on reducing them. These calls work on the caller's buffers alone: they use the context's device, stream and error
+ * message, none of its workspace or tables, and can be called in any order with the stages above and in a stream capture
+ * (they allocate nothing, copy nothing and never synchronise).
+ *
+ * sttm_cache describes a pool of pages. The row of head h, slot s of page p starts at element
+ * p*page_stride + h*head_stride + s*token_stride of k and of v and has head_dim elements. Requirements: head_dim % 8 == 0,
+ * 8 <= head_dim <= 256; page_size a power of two, 8 .. 1024; k, v and all strides multiples of 16 bytes; 1 <= kv_heads <=
+ * 1024; 1 <= pages < 2^31. */
+typedef struct {
+  void* k;  /* device */
+  void* v;  /* device */
+  int dtype; /* sttm_dtype of the rows */
+  int kv_heads, head_dim, page_size;
+  int64_t pages, page_stride, head_stride, token_stride;
+} sttm_cache;
+
+/* The sequences of a batch: slot i of sequence b is slot i % page_size of page block_table[b*table_stride + i/page_size].
+ * max_len: no length is above it (launches are sized by it; a length above it, or above the pages of a row, is read as if
+ * it were that, one below zero as zero). Entries of the table behind a sequence's last slot are not read. A page number
+ * outside the pool is not followed: its slots count as masked. batch <= 65535 (0: nothing is done). */
+typedef struct {
+  const int32_t* block_table; /* device [batch, max_pages] */
+  const int32_t* lengths;     /* device [batch] */
+  int64_t table_stride;       /* elements, >= max_pages */
+  int batch, max_pages, max_len;
+} sttm_sequences;
+
+/* A rotation by position. The first 2*(sections[0] + sections[1] + sections[2]) channels of a head form pairs: channels
+ * i and i + pairs, or with `interleaved` 2i and 2i + 1. Pair i turns by positions[row*pos_stride + axis]*inv_freq[i], axis
+ * = the section i falls into (one section: one position a row; three: (t, y, x), e.g. the root_tyxl of sttm_positions with
+ * pos_stride 4). The other channels stay. The number of pairs is a multiple of 4 (0: no rotation). positions: int32, or
+ * float (the merged_pos of sttm_positions) with pos_float. The angle is formed in 64 bits. */
+typedef struct {
+  const void* positions;  /* device */
+  const float* inv_freq;  /* device [pairs] */
+  int64_t pos_stride;     /* elements between rows */
+  int sections[3];
+  int pos_float, interleaved;
+} sttm_rope;
+
+/* Norm of queries and keys per head, rotation by position, and the write into the cache, in one pass. q [n, q_heads, d],
+ * k and v [n, kv_heads, d] (device; d = head_dim; the heads of a row one after the other, rows *_stride elements apart, so
+ * that parts of one projection's output can be named in place). A head's row x of q and k becomes
+ * x * weight / sqrt(mean(x^2) + eps) (weight: device [d] of the same type; NULL: x stays) and then turns (rope NULL: it does
+ * not); v is copied. Computed in fp32 and rounded once.
+ * q_out [n, q_heads, d], k_out [n, kv_heads, d]: rows *_out_stride apart, may be q and k themselves with their strides (k_out
+ * may be NULL). cache (or NULL): row i's key and value go to slot slots[i] (device int64: page*page_size + slot in the
+ * page); an entry that is no slot of the pool is skipped. Two rows must not name the same slot. cache NULL: v and slots
+ * may be NULL. q and k may not be NULL; n <= 2^25; q_heads >= 1, kv_heads >= 1, (q_heads + 2*kv_heads) <= 4096. All rows 16-byte
+ * aligned. dtype is the cache's. Asynchronous. */
+int sttm_qk_norm_rope(sttm_ctx* ctx, int dtype, int64_t n, int q_heads, int kv_heads, int head_dim, const void* q_dev,
+                      int64_t q_stride, const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                      const void* q_weight_dev, const void* k_weight_dev, float eps, const sttm_rope* rope,
+                      void* q_out_dev, int64_t q_out_stride, void* k_out_dev, int64_t k_out_stride,
+                      const sttm_cache* cache, const int64_t* slots_dev);
+
+/* Attention of one new token of every sequence over its cached keys. q, out [batch, q_heads, d] of the cache's type (rows
+ * q_stride / out_stride elements apart, 16-byte aligned); q_heads is a multiple of kv_heads, head h of q reads
+ * key-value head h / (q_heads / kv_heads), q_heads / kv_heads <= 256. With s_j = scale * (q . k_j) + key_bias_j:
+ *   out = sum_j softmax(s)_j v_j,   lse float [batch, q_heads] (may be NULL) = log sum_j exp(s_j),
+ *   weights_out_j = weights_in_j + sum over the heads of the group of softmax(s)_j.
+ * key_bias, weights_in, weights_out: float [batch, kv_heads, slot_stride], slot_stride >= max_len, entries from a sequence's
+ * length on neither read nor written. key_bias (or NULL): e.g. the log of the number of tokens a merged one stands for
+ * (counts of sttm_reduce); -inf masks a slot, whatever its key and value hold. weights_out NULL: weights are not wanted;
+ * weights_in NULL: zeros; weights_out may be weights_in. A query with no key left gets out = 0, lse = -inf and adds no weight.
+ * Sums and softmax in fp32. Results do not depend on what else runs, nor on the order of workgroups.
+ * workspace: sttm_paged_attention_workspace_bytes(...) bytes on the device, 256-byte aligned, overwritten at will; calls that
+ * overlap in time need one each. Asynchronous. */
+int sttm_paged_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* seqs, int q_heads, float scale,
+                         const void* q_dev, int64_t q_stride, const float* key_bias_dev, const float* weights_in_dev,
+                         float* weights_out_dev, int64_t slot_stride, void* out_dev, int64_t out_stride, float* lse_dev,
+                         void* workspace_dev, size_t workspace_bytes);
+/* Bytes for a call with weights_out (weights != 0) or without; 0 for descriptions that a call would refuse. */
+size_t sttm_paged_attention_workspace_bytes(const sttm_cache* cache, const sttm_sequences* seqs, int q_heads, int weights);
+
+/* Eviction by accumulated weight. Every slot of a (sequence, kv head) holds a token with a number: ids_in[slot], or where
+ * that is below zero total - length + slot (tokens appended one after the other since the last eviction; total int32
+ * [batch]: how many tokens the sequence has had, NULL = its length). keep int32 [batch] (device): the new length is
+ * min(length, max(keep, 0)). The slots that stay are the first ones in this order: numbers below `sink` or from
+ * total - recent on before all others; then the larger weights_in (NaN behind all numbers); then the lower number.
+ * The slots that stay but lie behind the new length move, in ascending order, into the slots before it whose tokens went,
+ * ascending: rows of k and v in the pool, and the entries of the tables. (Keys carry their positions, so that
+ * attention does not depend on the order of slots; as few rows move as can.) The pages behind the new length are free then.
+ * Tables: float weights_in/out and bias_in/out (bias both or neither NULL), int32 ids_in/out (ids_in NULL: all below zero),
+ * all [batch, kv_heads, slot_stride]; an output may be its input. Outputs: the tokens that stay, with their numbers; from the
+ * new length to the old one weight 0, number -1, bias 0; behind that as they were. lengths_out int32 [batch] (may be
+ * the lengths of seqs). No number may occur twice in one (sequence, kv head). Pages that several sequences share must
+ * not be among those that change. A slot whose page number lies outside the
+ * pool takes part in the order; its rows are not moved.
+ * workspace as for sttm_paged_attention, of sttm_cache_evict_workspace_bytes(...) bytes. Asynchronous. */
+int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* seqs, const int32_t* keep_dev,
+                     const int32_t* total_dev, int sink, int recent, int64_t slot_stride, const float* weights_in_dev,
+                     float* weights_out_dev, const int32_t* ids_in_dev, int32_t* ids_out_dev, const float* bias_in_dev,
+                     float* bias_out_dev, int32_t* lengths_out_dev, void* workspace_dev, size_t workspace_bytes);
+size_t sttm_cache_evict_workspace_bytes(const sttm_cache* cache, const sttm_sequences* seqs);
+
 /* ---- inspection ---------------------------------------------------------------------------------------- */
 
 /* Copies an internal table (device to device, asynchronous) into dst_dev; bytes must equal the table's size. */

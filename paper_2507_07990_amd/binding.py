@@ -30,11 +30,31 @@ EXPORTS = [
     "sttm_temporal_stats", "sttm_temporal_merge", "sttm_budget_threshold", "sttm_reduce", "sttm_export",
     "sttm_profile_enable", "sttm_profile_read", "sttm_set_match_mode", "sttm_set_output_order", "sttm_positions",
     "sttm_set_cell_dots", "sttm_invalidate", "sttm_reduce_noalloc", "sttm_reduce_noalloc_max_bytes",
-    "sttm_reduce_noalloc_bytes",
+    "sttm_reduce_noalloc_bytes", "sttm_qk_norm_rope", "sttm_paged_attention", "sttm_paged_attention_workspace_bytes",
+    "sttm_cache_evict", "sttm_cache_evict_workspace_bytes",
 ]
 STTM_MATCH_FIRST_PASSING, STTM_MATCH_TOPLEFT_ONLY, STTM_MATCH_MOST_SIMILAR = 0, 1, 2
 STTM_ORDER_RASTER, STTM_ORDER_ZSCAN = 0, 1
 STTM_KERNEL_PYRAMID_STATS, STTM_KERNEL_TEMPORAL_DOTS, STTM_KERNEL_REDUCE_GATHER = 0, 1, 2
+
+
+class _CacheStruct(C.Structure):
+    """sttm_cache"""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("page_size", C.c_int), ("pages", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64)]
+
+
+class _SequencesStruct(C.Structure):
+    """sttm_sequences"""
+    _fields_ = [("block_table", C.c_void_p), ("lengths", C.c_void_p), ("table_stride", C.c_int64), ("batch", C.c_int),
+                ("max_pages", C.c_int), ("max_len", C.c_int)]
+
+
+class _RopeStruct(C.Structure):
+    """sttm_rope"""
+    _fields_ = [("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("pos_stride", C.c_int64), ("sections", C.c_int * 3),
+                ("pos_float", C.c_int), ("interleaved", C.c_int)]
 
 
 def _load() -> C.CDLL:
@@ -42,7 +62,10 @@ def _load() -> C.CDLL:
         raise ImportError(
             f"{LIB_PATH} is missing: build it with `python -m paper_2507_07990_amd.build` "
             "(there is no CPU fallback)")
-    lib = C.CDLL(LIB_PATH)
+    return _declare(C.CDLL(LIB_PATH))
+
+
+def _declare(lib: C.CDLL) -> C.CDLL:
     vp, i, i64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
     lib.sttm_create.argtypes = [C.POINTER(vp), i, vp]
     lib.sttm_destroy.argtypes = [vp]
@@ -72,6 +95,14 @@ def _load() -> C.CDLL:
     lib.sttm_reduce_noalloc_bytes.argtypes = [i, i, i, i, i, i]
     lib.sttm_reduce_noalloc_bytes.restype = sz
     lib.sttm_positions.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, vp, vp]
+    f, cache, seqs, rope = C.c_float, C.POINTER(_CacheStruct), C.POINTER(_SequencesStruct), C.POINTER(_RopeStruct)
+    lib.sttm_qk_norm_rope.argtypes = [vp, i, i64, i, i, i, vp, i64, vp, i64, vp, i64, vp, vp, f, rope, vp, i64, vp, i64, cache, vp]
+    lib.sttm_paged_attention.argtypes = [vp, cache, seqs, i, f, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, sz]
+    lib.sttm_paged_attention_workspace_bytes.argtypes = [cache, seqs, i, i]
+    lib.sttm_paged_attention_workspace_bytes.restype = sz
+    lib.sttm_cache_evict.argtypes = [vp, cache, seqs, vp, vp, i, i, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz]
+    lib.sttm_cache_evict_workspace_bytes.argtypes = [cache, seqs]
+    lib.sttm_cache_evict_workspace_bytes.restype = sz
     return lib
 
 
@@ -102,6 +133,109 @@ def sttm_reduce_noalloc_max_bytes() -> int:
 
 def sttm_reduce_noalloc_bytes(B, T, H, W, D, dtype) -> int:
     return int(_lib.sttm_reduce_noalloc_bytes(B, T, H, W, D, dtype))
+
+
+_DTYPES = {torch.float32: STTM_F32, torch.bfloat16: STTM_BF16, torch.float16: STTM_F16}
+
+
+def _expect(ok: bool, code: int, msg: str):
+    if not ok:
+        raise SttmError(code, msg)
+
+
+class PagedCache:
+    """sttm_cache: keys and values, tensors [pages, kv_heads, page_size, head_dim] of one type and one set of strides (the
+    last one 1; e.g. two views of one buffer, or [pages, page_size, kv_heads, head_dim] with the middle axes exchanged)."""
+
+    def __init__(self, k, v):
+        _expect(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1, STTM_ERR_SHAPE,
+                "k and v must be [pages, kv_heads, page_size, head_dim] with the same strides, the last one 1")
+        _expect(k.dtype == v.dtype and k.dtype in _DTYPES, STTM_ERR_DTYPE, "k and v must be of one type, float32, bfloat16 or float16")
+        _expect(k.device == v.device, STTM_ERR_ARG, "k and v must be on one device")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        strides = [st if n > 1 else 0 for n, st in zip(k.shape, k.stride())]   # (the stride of a single entry means nothing)
+        self.struct = _CacheStruct(_ptr(k), _ptr(v), _DTYPES[k.dtype], self.kv_heads, self.head_dim, self.page_size, self.pages,
+                                   strides[0], strides[1], strides[2] or self.head_dim)
+
+
+class Sequences:
+    """sttm_sequences: block_table int32 [batch, max_pages] (rows any stride apart), lengths int32 [batch]; no length is above
+    max_len (default: the slots of a table row)."""
+
+    def __init__(self, block_table, lengths, max_len: Optional[int] = None):
+        _expect(block_table.dim() == 2 and lengths.dim() == 1 and block_table.shape[0] == lengths.shape[0], STTM_ERR_SHAPE,
+                "block_table must be [batch, max_pages], lengths [batch]")
+        _expect(block_table.dtype == torch.int32 and lengths.dtype == torch.int32, STTM_ERR_DTYPE, "block_table and lengths must be int32")
+        batch, pages = block_table.shape
+        _expect((pages <= 1 or block_table.stride(1) == 1) and (batch <= 1 or lengths.stride(0) == 1), STTM_ERR_SHAPE,
+                "the rows of block_table and lengths must be contiguous")
+        _expect(block_table.device == lengths.device, STTM_ERR_ARG, "block_table and lengths must be on one device")
+        _expect(max_len is None or max_len >= 0, STTM_ERR_SHAPE, "max_len must not be negative")
+        self.block_table, self.lengths, self.batch, self.device = block_table, lengths, batch, lengths.device
+        self.max_pages, self.max_len = pages, 2**31 - 1 if max_len is None else min(int(max_len), 2**31 - 1)
+        self.struct = _SequencesStruct(_ptr(block_table), _ptr(lengths), block_table.stride(0) if batch > 1 else pages, batch, pages,
+                                       self.max_len)
+
+
+class Rope:
+    """sttm_rope: positions int32 or float32 [n, axes or more] (or [n]: one axis), inv_freq float32 [pairs], sections: pairs
+    for each axis (default: all on the first)."""
+
+    def __init__(self, positions, inv_freq, sections: Optional[Sequence[int]] = None, interleaved: bool = False):
+        _expect(positions.dtype in (torch.int32, torch.float32) and inv_freq.dtype == torch.float32, STTM_ERR_DTYPE,
+                "positions must be int32 or float32, inv_freq float32")
+        _expect(inv_freq.dim() == 1 and (inv_freq.numel() <= 1 or inv_freq.stride(0) == 1), STTM_ERR_SHAPE, "inv_freq must be [pairs], contiguous")
+        if positions.dim() == 1:
+            positions = positions[:, None]
+        _expect(positions.dim() == 2 and (positions.shape[1] <= 1 or positions.stride(1) == 1), STTM_ERR_SHAPE,
+                "positions must be [n] or [n, axes] with contiguous rows")
+        parts = [inv_freq.numel()] if sections is None else [int(x) for x in sections]
+        _expect(1 <= len(parts) <= min(3, max(1, positions.shape[1])) and sum(parts) == inv_freq.numel() and min(parts) >= 0, STTM_ERR_SHAPE,
+                "sections: one to three numbers of pairs that add up to inv_freq's, no more of them than positions has axes")
+        _expect(positions.device == inv_freq.device, STTM_ERR_ARG, "positions and inv_freq must be on one device")
+        self.positions, self.inv_freq, self.device, self.n = positions, inv_freq, inv_freq.device, positions.shape[0]
+        stride = positions.stride(0) if self.n > 1 else positions.shape[1]
+        self.struct = _RopeStruct(_ptr(positions), _ptr(inv_freq), stride, (C.c_int * 3)(*parts, *[0] * (3 - len(parts))),
+                                  int(positions.dtype == torch.float32), int(interleaved))
+
+
+def sttm_paged_attention_workspace_bytes(cache: PagedCache, sequences: Sequences, q_heads: int, weights: bool = False) -> int:
+    return int(_lib.sttm_paged_attention_workspace_bytes(cache.struct, sequences.struct, q_heads, int(weights)))
+
+
+def sttm_cache_evict_workspace_bytes(cache: PagedCache, sequences: Sequences) -> int:
+    return int(_lib.sttm_cache_evict_workspace_bytes(cache.struct, sequences.struct))
+
+
+def _row_stride(t, name: str, n: int, like) -> int:
+    """The elements between the rows of t [n, heads, d], whose heads lie one after the other."""
+    shape, stride = t.shape, t.stride()
+    heads = shape[1] if len(shape) == 3 else 0
+    if (len(shape) != 3 or shape[0] != n or (heads > 1 and stride[1] != shape[2]) or (stride[2] != 1 and shape[2] > 1)):
+        raise SttmError(STTM_ERR_SHAPE, f"{name} must be [{n}, heads, head_dim], the heads of a row one after the other")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise SttmError(STTM_ERR_DTYPE, f"{name} must be of the type and on the device of the others")
+    return stride[0] if n > 1 else heads * shape[2]
+
+
+def _slot_table(t, name: str, dtype, shape, device):
+    """t [batch, kv_heads, slots], rows contiguous and evenly apart."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.device != device:
+        raise SttmError(STTM_ERR_DTYPE, f"{name} must be {dtype} on the cache's device")
+    if t.shape != shape or not t.is_contiguous():
+        raise SttmError(STTM_ERR_SHAPE, f"{name} must be [batch, kv_heads, slots], contiguous, with as many slots as the other tables")
+
+
+def _vector(t, name: str, dtype, n: int, device):
+    if t is None:
+        return
+    if t.dtype != dtype or t.device != device:
+        raise SttmError(STTM_ERR_DTYPE, f"{name} must be {dtype} on the device of the others")
+    if t.numel() != n or not t.is_contiguous():
+        raise SttmError(STTM_ERR_SHAPE, f"{name} must have {n} entries, contiguous")
 
 
 def _ptr(t) -> Optional[int]:
@@ -215,6 +349,90 @@ class Sttm:
         self._check(_lib.sttm_positions(self._h, _ptr(cluster_ids), _ptr(node_map), _ptr(node_level), _ptr(offsets),
                                         capacity,
                                         _ptr(survived), _ptr(reassigned), _ptr(merged_pos), _ptr(root_tyxl)))
+
+    # -- the reduced sequence in a model: a paged cache of keys and values -----------------------------
+    def _on_device(self, t):
+        if t.device.index != self.device:
+            raise SttmError(STTM_ERR_ARG, "the tensors must be on the context's device")
+
+    def sttm_qk_norm_rope(self, q, k, v, q_out, k_out=None, cache: Optional[PagedCache] = None, slots=None, q_weight=None,
+                          k_weight=None, eps: float = 1e-6, rope: Optional[Rope] = None):
+        """q [n, q_heads, d], k and v [n, kv_heads, d] (views of one projection's output will do); q_out, k_out of the same
+        shapes (or q and k themselves). cache, slots int64 [n]: where keys and values go."""
+        self._on_device(q)
+        n, q_heads, d = q.shape if q.dim() == 3 else (-1, 0, 0)
+        qs, ks, qos = _row_stride(q, "q", n, q), _row_stride(k, "k", n, q), _row_stride(q_out, "q_out", n, q)
+        kv_heads = k.shape[1]
+        if k.shape[2] != d or q_out.shape[1:] != (q_heads, d):
+            raise SttmError(STTM_ERR_SHAPE, "k must have q's head_dim, q_out q's shape")
+        vs = kos = 0
+        if k_out is not None:
+            kos = _row_stride(k_out, "k_out", n, q)
+            if k_out.shape[1:] != (kv_heads, d):
+                raise SttmError(STTM_ERR_SHAPE, "k_out must have k's shape")
+        if cache is not None:
+            vs = _row_stride(v, "v", n, q)
+            if v.shape[1:] != (kv_heads, d):
+                raise SttmError(STTM_ERR_SHAPE, "v must have k's shape")
+            if slots is None or cache.device != q.device:
+                raise SttmError(STTM_ERR_ARG, "a cache on the same device, and the rows' slots in it")
+            _vector(slots, "slots", torch.int64, n, q.device)
+        if rope is not None and (rope.n != n or rope.device != q.device):
+            raise SttmError(STTM_ERR_SHAPE, "the rotation must have a position for each row, on the same device")
+        _vector(q_weight, "q_weight", q.dtype, d, q.device)
+        _vector(k_weight, "k_weight", q.dtype, d, q.device)
+        if q.dtype not in _DTYPES:
+            raise SttmError(STTM_ERR_DTYPE, "float32, bfloat16 or float16")
+        self._check(_lib.sttm_qk_norm_rope(self._h, _DTYPES[q.dtype], n, q_heads, kv_heads, d, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs,
+                                           _ptr(q_weight), _ptr(k_weight), eps, rope.struct if rope is not None else None,
+                                           _ptr(q_out), qos, _ptr(k_out), kos, cache.struct if cache is not None else None, _ptr(slots)))
+
+    def sttm_paged_attention(self, q, cache: PagedCache, sequences: Sequences, out, scale: float, key_bias=None, weights_in=None,
+                             weights_out=None, lse=None, workspace=None):
+        """q, out [batch, q_heads, d]; key_bias, weights_in, weights_out float32 [batch, kv_heads, slots]; lse float32
+        [batch, q_heads]; workspace: sttm_paged_attention_workspace_bytes() bytes."""
+        self._on_device(q)
+        batch, dev = sequences.batch, q.device
+        qs, os_ = _row_stride(q, "q", batch, cache), _row_stride(out, "out", batch, cache)
+        q_heads = q.shape[1]
+        if q.shape[2] != cache.head_dim or out.shape != q.shape:
+            raise SttmError(STTM_ERR_SHAPE, "q must have the cache's head_dim, out q's shape")
+        if sequences.device != dev or (workspace is not None and workspace.device != dev):
+            raise SttmError(STTM_ERR_ARG, "the tensors must be on one device")
+        slots, first = 0, key_bias if key_bias is not None else weights_out
+        if first is not None:
+            slots = first.shape[-1]
+            shape = (batch, cache.kv_heads, slots)
+            _slot_table(key_bias, "key_bias", torch.float32, shape, dev)
+            _slot_table(weights_in, "weights_in", torch.float32, shape, dev)
+            _slot_table(weights_out, "weights_out", torch.float32, shape, dev)
+        _vector(lse, "lse", torch.float32, batch * q_heads, dev)
+        self._check(_lib.sttm_paged_attention(self._h, cache.struct, sequences.struct, q_heads, scale, _ptr(q), qs, _ptr(key_bias),
+                                              _ptr(weights_in), _ptr(weights_out), slots, _ptr(out), os_, _ptr(lse), _ptr(workspace),
+                                              workspace.nbytes if workspace is not None else 0))
+
+    def sttm_cache_evict(self, cache: PagedCache, sequences: Sequences, keep, lengths_out, weights_in, weights_out, ids_in, ids_out,
+                         total=None, sink: int = 0, recent: int = 0, bias_in=None, bias_out=None, workspace=None):
+        """keep, total, lengths_out int32 [batch]; weights_*, bias_* float32 and ids_* int32 [batch, kv_heads, slots];
+        workspace: sttm_cache_evict_workspace_bytes() bytes."""
+        self._on_device(cache)
+        batch, dev = sequences.batch, cache.device
+        if sequences.device != dev or (workspace is not None and workspace.device != dev):
+            raise SttmError(STTM_ERR_ARG, "the tensors must be on one device")
+        _vector(keep, "keep", torch.int32, batch, dev)
+        _vector(total, "total", torch.int32, batch, dev)
+        _vector(lengths_out, "lengths_out", torch.int32, batch, dev)
+        shape = (batch, cache.kv_heads, weights_in.shape[-1])
+        _slot_table(weights_in, "weights_in", torch.float32, shape, dev)
+        _slot_table(weights_out, "weights_out", torch.float32, shape, dev)
+        _slot_table(ids_in, "ids_in", torch.int32, shape, dev)
+        _slot_table(ids_out, "ids_out", torch.int32, shape, dev)
+        _slot_table(bias_in, "bias_in", torch.float32, shape, dev)
+        _slot_table(bias_out, "bias_out", torch.float32, shape, dev)
+        self._check(_lib.sttm_cache_evict(self._h, cache.struct, sequences.struct, _ptr(keep), _ptr(total), sink, recent, shape[2],
+                                          _ptr(weights_in), _ptr(weights_out), _ptr(ids_in), _ptr(ids_out), _ptr(bias_in),
+                                          _ptr(bias_out), _ptr(lengths_out), _ptr(workspace),
+                                          workspace.nbytes if workspace is not None else 0))
 
     def sttm_export(self, table, dst):
         self._check(_lib.sttm_export(self._h, table, _ptr(dst), dst.numel() * dst.element_size()))

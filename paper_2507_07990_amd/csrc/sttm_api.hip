@@ -1,5 +1,6 @@
 // C ABI of libsttm: argument checking, workspace layout, stage ordering. See include/sttm.h.
 #include "sttm_dev.h"
+#include "sttm_cache.h"
 #include "../../include/sttm.h"
 
 #include <cmath>
@@ -397,6 +398,16 @@ int check_feats(sttm_ctx* c, const void* feats) {
 }
 
 }  // namespace
+
+namespace sttm {
+int ctx_fail(sttm_ctx* c, int code, const char* msg) {
+  if (c) c->err.assign(msg);  // (short: within what is reserved)
+  return code;
+}
+int ctx_device(sttm_ctx* c) { return hip_check(c, hipSetDevice(c->device), "hipSetDevice"); }
+int ctx_after_launch(sttm_ctx* c) { return after_launch(c); }
+hipStream_t ctx_stream(const sttm_ctx* c) { return c->stream; }
+}  // namespace sttm
 
 extern "C" {
 

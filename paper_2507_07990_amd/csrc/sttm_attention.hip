@@ -1,0 +1,554 @@
+// Attention of one new token of every sequence over a paged cache, split over the cache's length and joined.
+#include "sttm_cache.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace sttm {
+namespace {
+
+constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
+constexpr int kQTile = 16;      // heads of a group that one matrix product takes
+constexpr int kChunkStep = 128; // a chunk is a multiple of this many slots: a block of 32 for each wavefront
+constexpr int kChunkMax = 1024;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+typedef float f32x4 __attribute__((vector_size(16)));
+typedef uint32_t u32x4 __attribute__((vector_size(16)));
+
+// ---- products on the matrix cores ---------------------------------------------------------------------------
+// D[m][n] += sum_k A[m][k] B[k][n], m, n < 16. A lane (i = lane % 16, g = lane / 16) holds A[i][*] and B[*][i] for the k of
+// its group g: eight 16-bit ones (v_mfma_f32_16x16x32) or one fp32 (v_mfma_f32_16x16x4), and D[4g + r][i], r < 4. Which k a
+// place stands for is free as long as A and B agree.
+#ifndef STTM_HOST_EMULATION
+template <int DT> __device__ inline f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+  typedef float v4 __attribute__((ext_vector_type(4)));
+  if constexpr (DT == 1) {
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), __builtin_bit_cast(v4, c), 0, 0, 0));
+  } else {
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), __builtin_bit_cast(v4, c), 0, 0, 0));
+  }
+}
+__device__ inline f32x4 mma32(float a, float b, f32x4 c) {
+  typedef float v4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, __builtin_bit_cast(v4, c), 0, 0, 0));
+}
+// (a's and b's 16-bit halves of one kind side by side, a's first)
+__device__ inline uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ inline uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+#else
+struct EmulOperands { u32x4 a[64], b[64]; };
+inline EmulOperands& emul_operands() {
+  static EmulOperands of_wave[16];
+  return of_wave[threadIdx.x >> 6];
+}
+template <int DT> inline f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+  EmulOperands& e = emul_operands();
+  const int lane = threadIdx.x & 63;
+  e.a[lane] = a;
+  e.b[lane] = b;
+  hip_emul::wave_sync();
+  for (int r = 0; r < 4; ++r) {
+    float sum = c[r];
+    for (int g = 0; g < 4; ++g)
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t x = e.a[g * 16 + 4 * (lane / 16) + r][w], y = e.b[g * 16 + lane % 16][w];
+        sum += low_half<DT>(x) * low_half<DT>(y) + high_half<DT>(x) * high_half<DT>(y);
+      }
+    c[r] = sum;
+  }
+  hip_emul::wave_sync();
+  return c;
+}
+inline f32x4 mma32(float a, float b, f32x4 c) {
+  EmulOperands& e = emul_operands();
+  const int lane = threadIdx.x & 63;
+  e.a[lane][0] = __float_as_uint(a);
+  e.b[lane][0] = __float_as_uint(b);
+  hip_emul::wave_sync();
+  for (int r = 0; r < 4; ++r)
+    for (int g = 0; g < 4; ++g)
+      c[r] += __uint_as_float(e.a[g * 16 + 4 * (lane / 16) + r][0]) * __uint_as_float(e.b[g * 16 + lane % 16][0]);
+  hip_emul::wave_sync();
+  return c;
+}
+inline uint32_t low_halves(uint32_t a, uint32_t b) { return (a & 0xffffu) | (b << 16); }
+inline uint32_t high_halves(uint32_t a, uint32_t b) { return (a >> 16) | (b & 0xffff0000u); }
+#endif
+
+struct AttnArgs {
+  Pool pool;
+  Seqs seqs;
+  const char* q;
+  char* out;
+  long long q_stride, out_stride;  // bytes
+  const float *bias, *weights_in;
+  float *weights_out, *lse;
+  long long slot_stride;
+  float* logits;     // [batch, kv_heads, max_len, group]: s_j in the units below (weights wanted), else NULL
+  float* part;       // [batch, q_heads, chunks, d]: unnormalised sums of the chunks (more than one chunk), else NULL
+  float2* stat;      // [batch, q_heads, chunks]: largest s and sum of exponentials of a chunk
+  float scale;       // of the product q.k: with unit = 1 the caller's times log2(e)
+  float natural;     // a unit of s, in natural logarithms: ln(2) or 1
+  float unit;        // s * unit is an exponent of two: 1, or log2(e) with a bias (s is then left as it is, since the lowest
+                     // fp32 number as a bias has no multiple)
+  int kv_heads, group, d, chunk, chunks, tiles;
+};
+
+// Softmax statistics of one head over several parts of the slots.
+__device__ inline float factor(float m, float top, float unit) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * unit); }
+
+// A slot's elements as one lane takes them: NV loads of 16 bytes (8 bytes: VW == 4 of 16 bits).
+template <int DT, int VW> struct ValueRow {
+  static constexpr int WORDS = DT == 0 ? VW : VW / 2;
+  uint32_t w[WORDS];
+  // `i`: lane % 16; bytes beyond the row are not read
+  __device__ inline void load(const char* row, int i, int bytes) {
+    if constexpr (DT != 0 && VW == 4) {
+      const int o = i * 8;
+      uint2 x = make_uint2(0u, 0u);
+      if (o < bytes) x = *reinterpret_cast<const uint2*>(row + o);
+      w[0] = x.x; w[1] = x.y;
+    } else {
+#pragma unroll
+      for (int h = 0; h < WORDS / 4; ++h) {
+        const int o = i * 16 + h * 256;
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (o < bytes) x = *reinterpret_cast<const uint4*>(row + o);
+        w[4 * h] = x.x; w[4 * h + 1] = x.y; w[4 * h + 2] = x.z; w[4 * h + 3] = x.w;
+      }
+    }
+  }
+  __device__ inline void clear() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+  }
+};
+
+// Where the sum of channel c (a multiple of 4; the three channels after it are 4 lines further each) is among what a
+// wavefront leaves in LDS, 64 * line + lane of head 0: lane m of sixteen holds a row's channels m*RUN .. in a load, channel
+// m*RUN + n is row m of product n, and row 4g + r of product n is line 4n + r of lanes 16g ...
+template <int DT, int VW> __device__ inline int value_place(int c) {
+  constexpr int RUN = DT == 0 || VW == 4 ? 4 : 8;
+  const int m = c % (16 * RUN) / RUN, n = c / (16 * RUN) * RUN + c % RUN;
+  return 64 * (4 * n + m % 4) + 16 * (m / 4);
+}
+
+template <int DT> __device__ inline void store_channels(char* at, const float (&x)[4]) {
+  if constexpr (DT == 0) *reinterpret_cast<float4*>(at) = make_float4(x[0], x[1], x[2], x[3]);
+  else *reinterpret_cast<uint2*>(at) = make_uint2(pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3]));
+}
+
+// One workgroup: one chunk of the slots of one (sequence, kv head, tile of 16 of the group's heads). Its wavefronts take
+// blocks of 32 slots (fp32: 16) in turn, each with its own running maximum and sum; at the end the four are joined in LDS.
+//
+// Both products are laid out so that nothing changes lanes between them: S = K Q^T has slots as rows and heads as columns,
+// a lane ends up with the slots 4g + r of each tile of 16 for head lane % 16; these are the k of its group in the second
+// product, O^T = V^T P^T, whose A operand a lane fills from the rows of the same slots, loaded as they lie in memory (16
+// lanes a row): channel lane * 8 + n is row `lane` of product n. The 16-bit transposition that is left is between registers
+// of one lane, one v_perm for two elements.
+//
+// P is handed on as the sum of two 16-bit numbers (16 bits of mantissa with bf16, 22 with fp16), one product each: rounding it to
+// one alone would cost as much accuracy as the result's own rounding.
+template <int DT, int NQ, int VW, bool BIAS>
+__global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
+  constexpr int ES = DT == 0 ? 4 : 2, TILES = DT == 0 ? 1 : 2, BLOCK = 16 * TILES, PART = VW < 8 ? VW : 8;
+  __shared__ long long page_at[kChunkMax / 8];        // byte offset of every page of the chunk, -1: not in the pool
+  __shared__ float joined[kAttnWaves][PART * 4][kWave];  // the wavefronts' sums, a part of the channels at a time
+  __shared__ float stat_m[kAttnWaves][kQTile], stat_l[kAttnWaves][kQTile];
+
+  const int b = blockIdx.z, h = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles, chunk = blockIdx.x;
+  const int length = seq_length(a.seqs, b);
+  const int first = chunk * a.chunk;
+  if (first >= length && chunk > 0) return;  // (an empty sequence's first chunk is gone through: its result is written)
+  const int end = min(length, first + a.chunk);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, i16 = lane & 15, g = lane >> 4;
+  const int head0 = tile * kQTile, heads = min(kQTile, a.group - head0);
+
+  for (int p = tid; p << a.pool.shift < end - first; p += kAttnThreads) {
+    const int page = a.seqs.table[b * a.seqs.table_stride + (first >> a.pool.shift) + p];
+    const bool ok = page >= 0 && page < a.pool.pages;
+    page_at[p] = ok ? page * a.pool.page_stride + h * a.pool.head_stride : -1;
+  }
+
+  // The tile's queries, as the B operand: column i16, the k of group g.
+  u32x4 q[NQ];
+  {
+    const char* row = a.q + b * a.q_stride + ((long long)h * a.group + head0 + min(i16, heads - 1)) * a.d * ES;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) {
+      const int o = (c * 4 + g) * 16;
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (i16 < heads && o < a.pool.row) x = *reinterpret_cast<const uint4*>(row + o);
+      q[c] = u32x4{x.x, x.y, x.z, x.w};
+    }
+  }
+  __syncthreads();
+
+  f32x4 acc[VW];
+#pragma unroll
+  for (int n = 0; n < VW; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;  // l: of this lane's slots
+  const int page_mask = (1 << a.pool.shift) - 1;
+  const float* bias = BIAS ? a.bias + ((long long)b * a.kv_heads + h) * a.slot_stride : nullptr;
+  float* logits = a.logits ? a.logits + ((long long)b * a.kv_heads + h) * a.seqs.max_len * a.group + head0 : nullptr;
+
+  for (int s0 = first + wave * BLOCK; s0 < end; s0 += kAttnWaves * BLOCK) {
+    // keys: lane i16 has the row of slot s0 + 16t + i16, its group's channels; values: slots s0 + 16t + 4g + r
+    u32x4 k[TILES][NQ];
+    ValueRow<DT, VW> v[TILES][4];
+    bool outside = false;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const int slot = min(s0 + 16 * t + i16, end - 1);
+      const long long at = page_at[(slot - first) >> a.pool.shift];
+      outside |= at < 0;
+      const char* row = a.pool.k + (at < 0 ? 0 : at) + (slot & page_mask) * a.pool.token_stride;
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) {
+        const int o = (c * 4 + g) * 16;
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (at >= 0 && o < a.pool.row) x = *reinterpret_cast<const uint4*>(row + o);
+        k[t][c] = u32x4{x.x, x.y, x.z, x.w};
+      }
+    }
+    const bool careful = BIAS || s0 + BLOCK > end || __ballot(outside) != 0;  // (the same in all lanes)
+    bool dead[TILES][4];
+    float add[TILES][4];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int slot = s0 + 16 * t + 4 * g + r, in = min(slot, end - 1);
+        const long long at = page_at[(in - first) >> a.pool.shift];
+        add[t][r] = BIAS ? bias[in] : 0.f;
+        dead[t][r] = careful && (slot >= end || at < 0 || add[t][r] == -INFINITY);
+        if (dead[t][r]) v[t][r].clear();
+        else v[t][r].load(a.pool.v + at + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
+      }
+    f32x4 s[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) {
+        if constexpr (DT == 0) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[t] = mma32(__uint_as_float(k[t][c][j]), __uint_as_float(q[c][j]), s[t]);
+        } else {
+          s[t] = mma16<DT>(k[t][c], q[c], s[t]);
+        }
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = BIAS ? fmaf(s[t][r], a.scale, add[t][r]) : s[t][r] * a.scale;
+        if (dead[t][r]) x = -INFINITY;
+        s[t][r] = x;
+        top = fmaxf(top, x);
+        if (logits && i16 < heads && s0 + 16 * t + 4 * g + r < end) logits[(long long)(s0 + 16 * t + 4 * g + r) * a.group + i16] = x;
+      }
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float m2 = fmaxf(m, top), base = m2 == -INFINITY ? 0.f : m2;
+    const float shrink = exp2_fast((m - base) * a.unit);
+    m = m2;
+    l *= shrink;
+#pragma unroll
+    for (int n = 0; n < VW; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[n][r] *= shrink;
+    float p[TILES][4];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[t][r] = exp2_fast((s[t][r] - base) * a.unit);
+        l += p[t][r];
+      }
+    if constexpr (DT == 0) {
+#pragma unroll
+      for (int n = 0; n < VW; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[n] = mma32(__uint_as_float(v[0][r].w[n]), p[0][r], acc[n]);
+    } else {
+      u32x4 hi, lo;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = p[j / 2][j % 2 * 2], y = p[j / 2][j % 2 * 2 + 1];
+        hi[j] = pack2<DT>(x, y);
+        lo[j] = pack2<DT>(x - low_half<DT>(hi[j]), y - high_half<DT>(hi[j]));
+      }
+#pragma unroll
+      for (int n = 0; n < VW; ++n) {
+        u32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t e = v[j / 2][j % 2 * 2].w[n / 2], f = v[j / 2][j % 2 * 2 + 1].w[n / 2];
+          x[j] = n % 2 ? high_halves(e, f) : low_halves(e, f);
+        }
+        acc[n] = mma16<DT>(x, hi, acc[n]);
+        acc[n] = mma16<DT>(x, lo, acc[n]);
+      }
+    }
+  }
+
+  // The wavefronts' sums on a common maximum, added up in their order.
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (lane < kQTile) {
+    stat_m[wave][lane] = m;
+    stat_l[wave][lane] = l;
+  }
+  __syncthreads();
+  float top = stat_m[0][i16];
+#pragma unroll
+  for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, stat_m[w][i16]);
+  const float mine = factor(m, top, a.unit);
+  float total = 0.f;
+#pragma unroll
+  for (int w = 0; w < kAttnWaves; ++w) total += stat_l[w][i16] * factor(stat_m[w][i16], top, a.unit);
+  const long long head = ((long long)b * a.kv_heads + h) * a.group + head0 + i16;
+  if (tid < heads) {
+    if (a.stat) a.stat[head * a.chunks + chunk] = make_float2(top, total);
+    if (!a.part && a.lse) a.lse[head] = top == -INFINITY ? -INFINITY : top * a.natural + logf(total);
+  }
+  const float share = a.part ? 1.f : total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int n0 = 0; n0 < VW; n0 += PART) {
+    if (n0) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < PART; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) joined[wave][n * 4 + r][lane] = acc[n0 + n][r] * mine;
+    __syncthreads();
+    // four channels a thread, head i16 as before
+    for (int u = tid >> 4; u < 4 * PART; u += kAttnThreads / 16) {
+      const int channel = 16 * n0 + 4 * u, place = value_place<DT, VW>(4 * u);
+      if (i16 >= heads || channel >= a.d) continue;
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) x[e] += joined[w][(place >> 6) + 4 * e][(place & 63) + i16];
+        x[e] *= share;
+      }
+      if (a.part) *reinterpret_cast<float4*>(a.part + (head * a.chunks + chunk) * a.d + channel) = make_float4(x[0], x[1], x[2], x[3]);
+      else store_channels<DT>(a.out + b * a.out_stride + (((long long)h * a.group + head0 + i16) * a.d + channel) * ES, x);
+    }
+  }
+}
+
+// Maximum and sum of one head over its chunks, by one wavefront.
+__device__ inline float2 join_stats(const float2* stat, int chunks, float unit, int lane) {
+  float top = -INFINITY, total = 0.f;
+  for (int c = lane; c < chunks; c += kWave) top = fmaxf(top, stat[c].x);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  for (int c = lane; c < chunks; c += kWave) total += stat[c].y * factor(stat[c].x, top, unit);
+  return make_float2(top, wave_sum(total));
+}
+
+// The chunks' sums on a common maximum: one workgroup a head, four channels a thread, the chunks dealt out among as many
+// groups of threads as there are; added up in a fixed order.
+constexpr int kJoinThreads = 256;
+template <int DT>
+__global__ void __launch_bounds__(kJoinThreads) k_attention_join(AttnArgs a) {
+  __shared__ float4 sums[kJoinThreads];
+  __shared__ float share[kJoinThreads];
+  __shared__ float2 all;
+  constexpr int ES = DT == 0 ? 4 : 2;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const long long head = (long long)b * a.kv_heads * a.group + h;
+  const int chunks = (seq_length(a.seqs, b) + a.chunk - 1) / a.chunk;
+  const float2* stat = a.stat + head * a.chunks;
+  if (tid < kWave) {
+    const float2 r = join_stats(stat, chunks, a.unit, tid);
+    if (tid == 0) {
+      all = r;
+      if (a.lse) a.lse[head] = r.x == -INFINITY ? -INFINITY : r.x * a.natural + logf(r.y);
+    }
+  }
+  __syncthreads();
+  const float top = all.x, total = all.y;
+  const int units = a.d / 4, slices = kJoinThreads / units, unit = tid % units, slice = tid / units;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c0 = 0; c0 < chunks; c0 += kJoinThreads) {
+    if (c0 + tid < chunks) share[tid] = factor(stat[c0 + tid].x, top, a.unit);
+    __syncthreads();
+    if (slice < slices)
+      for (int c = slice; c < min(kJoinThreads, chunks - c0); c += slices) {
+        const float4 y = *reinterpret_cast<const float4*>(a.part + (head * a.chunks + c0 + c) * a.d + 4 * unit);
+        const float f = share[c];
+        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+      }
+    __syncthreads();
+  }
+  sums[tid] = x;
+  __syncthreads();
+  if (slice != 0) return;
+  for (int i = 1; i < slices; ++i) {
+    const float4 y = sums[i * units + unit];
+    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+  }
+  const float inverse = total == 0.f ? 0.f : 1.f / total;
+  const float y[4] = {x.x * inverse, x.y * inverse, x.z * inverse, x.w * inverse};
+  store_channels<DT>(a.out + b * a.out_stride + ((long long)h * a.d + 4 * unit) * ES, y);
+}
+
+// Every slot's weight, summed over the group's heads, from the stored s.
+constexpr int kWeightThreads = 256, kWeightSlots = 1024;
+__global__ void __launch_bounds__(kWeightThreads) k_attention_weights(AttnArgs a) {
+  __shared__ float top[256], inverse[256];
+  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+  const int length = seq_length(a.seqs, b), first = blockIdx.x * kWeightSlots;
+  if (first >= length) return;
+  const long long row = (long long)b * a.kv_heads + h;
+  const int chunks = (length + a.chunk - 1) / a.chunk;
+  for (int q = tid / kWave; q < a.group; q += kWeightThreads / kWave) {
+    const float2 r = join_stats(a.stat + (row * a.group + q) * a.chunks, chunks, a.unit, tid & 63);
+    if ((tid & 63) == 0) {
+      top[q] = r.x == -INFINITY ? 0.f : r.x;
+      inverse[q] = r.y == 0.f ? 0.f : 1.f / r.y;
+    }
+  }
+  __syncthreads();
+  for (int slot = first + tid; slot < min(length, first + kWeightSlots); slot += kWeightThreads) {
+    const float* x = a.logits + (row * a.seqs.max_len + slot) * a.group;
+    float sum = 0.f;
+    for (int q = 0; q < a.group; ++q) sum = fmaf(exp2_fast((x[q] - top[q]) * a.unit), inverse[q], sum);
+    const long long at = row * a.slot_stride + slot;
+    a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
+  }
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------
+
+struct Plan {
+  int tiles, chunk, chunks;
+  size_t part, stat, logits, bytes;  // offsets in the workspace
+};
+
+Plan make_plan(const sttm_cache* c, const sttm_sequences* s, int q_heads, bool weights) {
+  Plan p;
+  const int group = q_heads / c->kv_heads, max_len = make_seqs(c, s).max_len;
+  p.tiles = (group + kQTile - 1) / kQTile;
+  // Chunks for some 1024 workgroups, if there are as many slots.
+  const long long rows = (long long)std::max(s->batch, 1) * c->kv_heads * p.tiles;
+  const long long want = std::max(1ll, 1024 / rows), len = std::max(max_len, 1);
+  long long chunk = ((len + want - 1) / want + kChunkStep - 1) / kChunkStep * kChunkStep;
+  p.chunk = (int)std::min(chunk, (long long)kChunkMax);
+  p.chunks = (int)((len + p.chunk - 1) / p.chunk);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
+  const size_t heads = (size_t)s->batch * q_heads;
+  p.part = take(p.chunks > 1 ? heads * p.chunks * c->head_dim * sizeof(float) : 0);
+  p.stat = take(p.chunks > 1 || weights ? heads * p.chunks * sizeof(float2) : 0);
+  p.logits = take(weights ? heads * (size_t)max_len * sizeof(float) : 0);
+  p.bytes = std::max(off, (size_t)256);
+  return p;
+}
+
+int check_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* seqs, int q_heads) {
+  int rc = check_cache(ctx, cache);
+  if (rc == STTM_OK) rc = check_sequences(ctx, cache, seqs);
+  if (rc != STTM_OK) return rc;
+  if (q_heads < 1 || q_heads % cache->kv_heads || q_heads / cache->kv_heads > 256 || q_heads > 65535)
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "need q_heads a multiple of kv_heads, at most 256 a kv head, q_heads <= 65535");
+  if ((double)seqs->batch * q_heads * seqs->max_len > 1e14) return ctx_fail(ctx, STTM_ERR_SHAPE, "batch * q_heads * max_len too large");
+  return STTM_OK;
+}
+
+template <int DT, int NQ, int VW>
+void launch_blocks(const AttnArgs& a, dim3 grid, hipStream_t s) {
+  if (a.bias) hipLaunchKernelGGL((k_paged_attention<DT, NQ, VW, true>), grid, dim3(kAttnThreads), 0, s, a);
+  else hipLaunchKernelGGL((k_paged_attention<DT, NQ, VW, false>), grid, dim3(kAttnThreads), 0, s, a);
+}
+
+// One instance for each way a head's channels fill the products: 64 bytes of a key and 16 lanes' shares of a value.
+template <int DT>
+void launch_attention(const AttnArgs& a, int batch, hipStream_t s) {
+  const dim3 grid(a.chunks, a.kv_heads * a.tiles, batch);
+  constexpr int W = DT == 0 ? 2 : 1;  // fp32 rows have twice the bytes
+  if (a.d <= 32) launch_blocks<DT, W, 4>(a, grid, s);
+  else if (a.d <= 64) launch_blocks<DT, 2 * W, 4>(a, grid, s);
+  else if (a.d <= 96) launch_blocks<DT, 3 * W, 8>(a, grid, s);
+  else if (a.d <= 128) launch_blocks<DT, 4 * W, 8>(a, grid, s);
+  else if (a.d <= 192) launch_blocks<DT, 6 * W, 16>(a, grid, s);
+  else launch_blocks<DT, 8 * W, 16>(a, grid, s);
+  if (a.part) hipLaunchKernelGGL((k_attention_join<DT>), dim3(a.kv_heads * a.group, batch), dim3(kJoinThreads), 0, s, a);
+}
+
+}  // namespace
+}  // namespace sttm
+
+using namespace sttm;
+
+extern "C" size_t sttm_paged_attention_workspace_bytes(const sttm_cache* cache, const sttm_sequences* seqs, int q_heads, int weights) {
+  if (check_attention(nullptr, cache, seqs, q_heads) != STTM_OK) return 0;
+  return make_plan(cache, seqs, q_heads, weights != 0).bytes;
+}
+
+extern "C" int sttm_paged_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* seqs, int q_heads, float scale,
+                                    const void* q, int64_t q_stride, const float* key_bias, const float* weights_in,
+                                    float* weights_out, int64_t slot_stride, void* out, int64_t out_stride, float* lse,
+                                    void* workspace, size_t workspace_bytes) {
+  if (!ctx) return STTM_ERR_NULL;
+  int rc = check_attention(ctx, cache, seqs, q_heads);
+  if (rc != STTM_OK) return rc;
+  const int es = elem_bytes(cache->dtype), align = 16 / es;
+  const int64_t row = (int64_t)q_heads * cache->head_dim, most = (int64_t)1 << 40;
+  if (q_stride < row || out_stride < row || q_stride > most || out_stride > most || q_stride % align || out_stride % align)
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "q_stride, out_stride: multiples of 16 bytes, no less than a row");
+  AttnArgs a{};
+  a.seqs = make_seqs(cache, seqs);
+  if ((key_bias || weights_out) && (slot_stride < a.seqs.max_len || slot_stride > most))
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "slot_stride must be no less than max_len");
+  if (!(std::fabs(scale) <= 3e38f)) return ctx_fail(ctx, STTM_ERR_ARG, "scale must be a finite number");
+  if (weights_in && !weights_out) return ctx_fail(ctx, STTM_ERR_ARG, "weights_in without weights_out");
+  if (seqs->batch == 0) return STTM_OK;
+  if (!q || !out) return ctx_fail(ctx, STTM_ERR_NULL, "q or out is NULL");
+  if (!aligned16(q) || !aligned16(out)) return ctx_fail(ctx, STTM_ERR_ARG, "q and out must be 16-byte aligned");
+  const Plan p = make_plan(cache, seqs, q_heads, weights_out != nullptr);
+  rc = check_workspace(ctx, workspace, workspace_bytes, p.bytes);
+  if (rc != STTM_OK) return rc;
+  char* ws = static_cast<char*>(workspace);
+  a.pool = make_pool(cache);
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.q_stride = q_stride * es;
+  a.out_stride = out_stride * es;
+  a.bias = key_bias;
+  a.weights_in = weights_in;
+  a.weights_out = weights_out;
+  a.lse = lse;
+  a.slot_stride = slot_stride;
+  if (weights_out) a.logits = reinterpret_cast<float*>(ws + p.logits);
+  if (p.chunks > 1) a.part = reinterpret_cast<float*>(ws + p.part);
+  if (p.chunks > 1 || weights_out) a.stat = reinterpret_cast<float2*>(ws + p.stat);
+  a.unit = key_bias ? kLog2e : 1.f;
+  a.natural = key_bias ? 1.f : kLn2;
+  a.scale = key_bias ? scale : scale * kLog2e;
+  a.kv_heads = cache->kv_heads;
+  a.group = q_heads / cache->kv_heads;
+  a.d = cache->head_dim;
+  a.chunk = p.chunk;
+  a.chunks = p.chunks;
+  a.tiles = p.tiles;
+  rc = ctx_device(ctx);
+  if (rc != STTM_OK) return rc;
+  const hipStream_t s = ctx_stream(ctx);
+  if (cache->dtype == STTM_F32) launch_attention<0>(a, seqs->batch, s);
+  else if (cache->dtype == STTM_BF16) launch_attention<1>(a, seqs->batch, s);
+  else launch_attention<2>(a, seqs->batch, s);
+  if (weights_out && a.seqs.max_len)
+    hipLaunchKernelGGL(k_attention_weights, dim3((a.seqs.max_len + kWeightSlots - 1) / kWeightSlots, a.kv_heads, seqs->batch),
+                       dim3(kWeightThreads), 0, s, a);
+  return ctx_after_launch(ctx);
+}

@@ -1,0 +1,8 @@
+// What the operators on a paged cache use beyond hip_runtime.h of this folder.
+#pragma once
+#include <hip/hip_runtime.h>
+
+struct float2 { float x, y; };
+struct int2 { int x, y; };
+inline float2 make_float2(float a, float b) { return {a, b}; }
+inline int2 make_int2(int a, int b) { return {a, b}; }
