@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         k[t][c] = u32x4{x.x, x.y, x.z, x.w};
       }
     }
-    const bool careful = BIAS || s0 + BLOCK > end || __ballot(outside) != 0;  // (the same in all lanes)
+    const bool careful = BIAS || s0 + BLOCK > end || __ballot(outside) != 0;  // (the same in all lanes: masked slots among these)
     bool dead[TILES][4];
     float add[TILES][4];
 #pragma unroll
@@ -224,9 +224,8 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         const int slot = s0 + 16 * t + 4 * g + r, in = min(slot, end - 1);
         const long long at = page_at[(in - first) >> a.pool.shift];
         add[t][r] = BIAS ? bias[in] : 0.f;
-        dead[t][r] = careful && (slot >= end || at < 0 || add[t][r] == -INFINITY);
-        if (dead[t][r]) v[t][r].clear();
-        else v[t][r].load(a.pool.v + at + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
+        dead[t][r] = slot >= end || at < 0;
+        v[t][r].load(a.pool.v + (at < 0 ? 0 : at) + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
       }
     f32x4 s[TILES];
 #pragma unroll
@@ -242,13 +241,22 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         }
       }
     }
+    if (careful) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          dead[t][r] |= add[t][r] == -INFINITY;
+          if (dead[t][r]) v[t][r].clear();
+        }
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float x = BIAS ? fmaf(s[t][r], a.scale, add[t][r]) : s[t][r] * a.scale;
-        if (dead[t][r]) x = -INFINITY;
+        if (careful && dead[t][r]) x = -INFINITY;
         s[t][r] = x;
         top = fmaxf(top, x);
         if (logits && i16 < heads && s0 + 16 * t + 4 * g + r < end) logits[(long long)(s0 + 16 * t + 4 * g + r) * a.group + i16] = x;
@@ -345,50 +353,52 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
   }
 }
 
-// Maximum and sum of one head over its chunks, by one wavefront.
+// Maximum and sum of one head over its chunks, the same in all lanes of a wavefront.
 __device__ inline float2 join_stats(const float2* stat, int chunks, float unit, int lane) {
   float top = -INFINITY, total = 0.f;
-  for (int c = lane; c < chunks; c += kWave) top = fmaxf(top, stat[c].x);
+  for (int c0 = 0; c0 < chunks; c0 += 4 * kWave) {
+    float2 x[4];
+    float most = top;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  for (int c = lane; c < chunks; c += kWave) total += stat[c].y * factor(stat[c].x, top, unit);
-  return make_float2(top, wave_sum(total));
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + k * kWave + lane;
+      x[k] = c < chunks ? stat[c] : make_float2(-INFINITY, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) most = fmaxf(most, x[k].x);
+    total *= factor(top, most, unit);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) total = fmaf(x[k].y, factor(x[k].x, most, unit), total);
+    top = most;
+  }
+  float all = top;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+  return make_float2(all, wave_sum(total * factor(top, all, unit)));
 }
 
-// The chunks' sums on a common maximum: one workgroup a head, four channels a thread, the chunks dealt out among as many
-// groups of threads as there are; added up in a fixed order.
-constexpr int kJoinThreads = 256;
-template <int DT>
-__global__ void __launch_bounds__(kJoinThreads) k_attention_join(AttnArgs a) {
-  __shared__ float4 sums[kJoinThreads];
-  __shared__ float share[kJoinThreads];
-  __shared__ float2 all;
+constexpr int kFinishThreads = 256;
+
+// The chunks' sums of one head on a common maximum: four channels a thread, the chunks dealt out among as many groups of
+// threads as there are, added up in a fixed order.
+template <int DT> __device__ inline void join_head(const AttnArgs& a, int b, int h, float4* sums) {
   constexpr int ES = DT == 0 ? 4 : 2;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const long long head = (long long)b * a.kv_heads * a.group + h;
   const int chunks = (seq_length(a.seqs, b) + a.chunk - 1) / a.chunk;
   const float2* stat = a.stat + head * a.chunks;
-  if (tid < kWave) {
-    const float2 r = join_stats(stat, chunks, a.unit, tid);
-    if (tid == 0) {
-      all = r;
-      if (a.lse) a.lse[head] = r.x == -INFINITY ? -INFINITY : r.x * a.natural + logf(r.y);
-    }
-  }
-  __syncthreads();
-  const float top = all.x, total = all.y;
-  const int units = a.d / 4, slices = kJoinThreads / units, unit = tid % units, slice = tid / units;
+  const float2 all = join_stats(stat, chunks, a.unit, tid & 63);
+  if (tid == 0 && a.lse) a.lse[head] = all.x == -INFINITY ? -INFINITY : all.x * a.natural + logf(all.y);
+  const int units = a.d / 4, slices = kFinishThreads / units, unit = tid % units, slice = tid / units;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c0 = 0; c0 < chunks; c0 += kJoinThreads) {
-    if (c0 + tid < chunks) share[tid] = factor(stat[c0 + tid].x, top, a.unit);
-    __syncthreads();
-    if (slice < slices)
-      for (int c = slice; c < min(kJoinThreads, chunks - c0); c += slices) {
-        const float4 y = *reinterpret_cast<const float4*>(a.part + (head * a.chunks + c0 + c) * a.d + 4 * unit);
-        const float f = share[c];
-        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
-      }
-    __syncthreads();
+  if (slice < slices) {
+    const float* part = a.part + head * a.chunks * a.d + 4 * unit;
+#pragma unroll 8
+    for (int c = slice; c < chunks; c += slices) {
+      const float4 y = *reinterpret_cast<const float4*>(part + (long long)c * a.d);
+      const float f = factor(stat[c].x, all.x, a.unit);
+      x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+    }
   }
   sums[tid] = x;
   __syncthreads();
@@ -397,35 +407,46 @@ __global__ void __launch_bounds__(kJoinThreads) k_attention_join(AttnArgs a) {
     const float4 y = sums[i * units + unit];
     x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
   }
-  const float inverse = total == 0.f ? 0.f : 1.f / total;
+  const float inverse = all.y == 0.f ? 0.f : 1.f / all.y;
   const float y[4] = {x.x * inverse, x.y * inverse, x.z * inverse, x.w * inverse};
   store_channels<DT>(a.out + b * a.out_stride + ((long long)h * a.d + 4 * unit) * ES, y);
 }
 
-// Every slot's weight, summed over the group's heads, from the stored s.
-constexpr int kWeightThreads = 256, kWeightSlots = 1024;
-__global__ void __launch_bounds__(kWeightThreads) k_attention_weights(AttnArgs a) {
-  __shared__ float top[256], inverse[256];
-  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
-  const int length = seq_length(a.seqs, b), first = blockIdx.x * kWeightSlots;
+// The weights of some slots of one kv head, summed over the group's heads, from the stored s: one slot a thread. The first
+// few s are on their way while the statistics are put together.
+__device__ inline void add_weights(const AttnArgs& a, int b, int h, int first, float2* of_head) {
+  constexpr int AHEAD = 8;
+  const int tid = threadIdx.x, length = seq_length(a.seqs, b);
   if (first >= length) return;
   const long long row = (long long)b * a.kv_heads + h;
-  const int chunks = (length + a.chunk - 1) / a.chunk;
-  for (int q = tid / kWave; q < a.group; q += kWeightThreads / kWave) {
+  const int chunks = (length + a.chunk - 1) / a.chunk, slot = min(first + tid, length - 1);
+  const float* x = a.logits + (row * a.seqs.max_len + slot) * a.group;
+  const long long at = row * a.slot_stride + slot;
+  float ahead[AHEAD], before = 0.f;
+#pragma unroll
+  for (int q = 0; q < AHEAD; ++q) ahead[q] = x[min(q, a.group - 1)];
+  if (a.weights_in) before = a.weights_in[at];
+  for (int q = tid / kWave; q < a.group; q += kFinishThreads / kWave) {
     const float2 r = join_stats(a.stat + (row * a.group + q) * a.chunks, chunks, a.unit, tid & 63);
-    if ((tid & 63) == 0) {
-      top[q] = r.x == -INFINITY ? 0.f : r.x;
-      inverse[q] = r.y == 0.f ? 0.f : 1.f / r.y;
-    }
+    if ((tid & 63) == 0) of_head[q] = make_float2(r.x == -INFINITY ? 0.f : r.x, r.y == 0.f ? 0.f : 1.f / r.y);
   }
   __syncthreads();
-  for (int slot = first + tid; slot < min(length, first + kWeightSlots); slot += kWeightThreads) {
-    const float* x = a.logits + (row * a.seqs.max_len + slot) * a.group;
-    float sum = 0.f;
-    for (int q = 0; q < a.group; ++q) sum = fmaf(exp2_fast((x[q] - top[q]) * a.unit), inverse[q], sum);
-    const long long at = row * a.slot_stride + slot;
-    a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
-  }
+  float sum = 0.f;
+#pragma unroll
+  for (int q = 0; q < AHEAD; ++q)
+    if (q < a.group) sum = fmaf(exp2_fast((ahead[q] - of_head[q].x) * a.unit), of_head[q].y, sum);
+  for (int q = AHEAD; q < a.group; ++q) sum = fmaf(exp2_fast((x[q] - of_head[q].x) * a.unit), of_head[q].y, sum);
+  if (first + tid < length) a.weights_out[at] = before + sum;
+}
+
+// What is left when every chunk is done: blocks 0 .. joins - 1 of a kv head put its heads' sums together, the others add the
+// weights up.
+template <int DT>
+__global__ void __launch_bounds__(kFinishThreads) k_attention_finish(AttnArgs a, int joins) {
+  __shared__ float4 shared[kFinishThreads];
+  const int x = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  if (x < joins) join_head<DT>(a, b, h * a.group + x, shared);
+  else add_weights(a, b, h, (x - joins) * kFinishThreads, reinterpret_cast<float2*>(shared));
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------
@@ -482,7 +503,9 @@ void launch_attention(const AttnArgs& a, int batch, hipStream_t s) {
   else if (a.d <= 128) launch_blocks<DT, 4 * W, 8>(a, grid, s);
   else if (a.d <= 192) launch_blocks<DT, 6 * W, 16>(a, grid, s);
   else launch_blocks<DT, 8 * W, 16>(a, grid, s);
-  if (a.part) hipLaunchKernelGGL((k_attention_join<DT>), dim3(a.kv_heads * a.group, batch), dim3(kJoinThreads), 0, s, a);
+  const int joins = a.part ? a.group : 0, weights = a.weights_out ? (a.seqs.max_len + kFinishThreads - 1) / kFinishThreads : 0;
+  if (joins + weights)
+    hipLaunchKernelGGL((k_attention_finish<DT>), dim3(joins + weights, a.kv_heads, batch), dim3(kFinishThreads), 0, s, a, joins);
 }
 
 }  // namespace
@@ -547,8 +570,5 @@ extern "C" int sttm_paged_attention(sttm_ctx* ctx, const sttm_cache* cache, cons
   if (cache->dtype == STTM_F32) launch_attention<0>(a, seqs->batch, s);
   else if (cache->dtype == STTM_BF16) launch_attention<1>(a, seqs->batch, s);
   else launch_attention<2>(a, seqs->batch, s);
-  if (weights_out && a.seqs.max_len)
-    hipLaunchKernelGGL(k_attention_weights, dim3((a.seqs.max_len + kWeightSlots - 1) / kWeightSlots, a.kv_heads, seqs->batch),
-                       dim3(kWeightThreads), 0, s, a);
   return ctx_after_launch(ctx);
 }

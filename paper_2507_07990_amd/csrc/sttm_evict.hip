@@ -6,12 +6,6 @@
 namespace sttm {
 namespace {
 
-// A survivor from behind the new length, with its entries in the tables.
-struct Mover {
-  int32_t slot, id;
-  float weight, bias;
-};
-
 struct EvictArgs {
   Pool pool;
   Seqs seqs;
@@ -22,146 +16,388 @@ struct EvictArgs {
   float *weights_out, *bias_out;
   int32_t *ids_out, *lengths_out;
   int kv_heads, sink, recent;
-  Mover* movers;    // [batch, kv_heads, max_len]
-  int32_t* holes;   // [batch, kv_heads, max_len]
-  int2* counts;     // [batch, kv_heads]: movers (= holes), new length
+  uint32_t* keys;              // [batch, kv_heads, max_len], of long rows, and
+  unsigned short* digits;      // [batch, kv_heads, parts, 1024]: counts of their top digits
+  unsigned long long* stays;   // [batch, kv_heads, words]: a bit a slot
+  int32_t *holes, *movers;     // [batch, kv_heads, pairs]: the j-th mover goes to the j-th hole
+  int4* counts;                // [batch, kv_heads]: pairs, new length, length, tokens so far (seqs.lengths may be lengths_out)
+  int words, pairs, parts;
 };
 
-// The order of the slots as a 64-bit number, larger ones stay: the class and weight, then the lower number.
-__device__ inline unsigned long long rank_key(float w, int id, int total, const EvictArgs& a) {
-  unsigned hi;
-  if (id < a.sink || (long long)id >= (long long)total - a.recent) hi = 0xffffffffu;
-  else if (w != w) hi = 0u;
-  else hi = float_key(w == 0.f ? 0.f : w);   // (0x007fffff .. 0xff800000; both zeros alike)
-  return (unsigned long long)hi << 32 | ~(unsigned)id;
+__device__ inline int slot_number(const EvictArgs& a, long long at, int i, int length, int total) {
+  const int id = a.ids_in ? a.ids_in[at + i] : -1;
+  return id < 0 ? total - length + i : id;
+}
+
+// The order of the slots: larger ones stay, equal ones by the lower number. Protected slots are above all weights, NaN
+// below (float_key has numbers in 0x007fffff .. 0xff800000); both zeros are alike.
+__device__ inline uint32_t weight_key(float w, int id, int total, const EvictArgs& a) {
+  if (id < a.sink || (long long)id >= (long long)total - a.recent) return 0xffffffffu;
+  return w != w ? 0u : float_key(w == 0.f ? 0.f : w);
 }
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;  // a digit's count a thread
+constexpr int kListMost = 4096;                            // keys that fit the list in LDS
+constexpr int kPartThreads = 256, kPartSlots = 4096;       // of one workgroup that works out keys
+constexpr int kKeysHere = 8;                               // keys a lane of a row that is gone through by one workgroup alone
 
-// One workgroup a (sequence, kv head). The new length's largest keys are found digit by digit from the top (eight bits a
-// pass, until the digits so far cut off exactly as many as stay); one more pass deals out holes and movers in the order of
-// their slots and writes the tables.
+// GROUP keys of a lane, 64 slots apart from `from` on; all loads under way together.
+template <int GROUP>
+__device__ inline void keys_of(const EvictArgs& a, long long at, int from, int length, int total, uint32_t (&out)[GROUP]) {
+  float w[GROUP];
+  int id[GROUP];
+#pragma unroll
+  for (int k = 0; k < GROUP; ++k) {
+    const int i = min(from + k * kWave, length - 1);
+    w[k] = a.weights_in[at + i];
+    id[k] = a.ids_in ? a.ids_in[at + i] : -1;
+  }
+#pragma unroll
+  for (int k = 0; k < GROUP; ++k) {
+    const int i = min(from + k * kWave, length - 1);
+    out[k] = weight_key(w[k], id[k] < 0 ? total - length + i : id[k], total, a);
+  }
+}
+
+// Counts a digit of every lane with `mine` set (all lanes call). Lanes that agree with the first one are counted in one
+// step: many weights are alike where nothing was looked at.
+__device__ inline void count_digit(unsigned* hist, bool mine, uint32_t digit, int lane) {
+  const unsigned long long any = __ballot(mine);
+  if (!any) return;
+  const int leader = __ffsll((long long)any) - 1;
+  const uint32_t of_leader = (uint32_t)lane_value((int)digit, leader);
+  const unsigned long long same = __ballot(mine && digit == of_leader);
+  if (lane == leader) atomicAdd(&hist[digit], (unsigned)__popcll(same));
+  else if (mine && !(same >> lane & 1)) atomicAdd(&hist[digit], 1u);
+}
+
+// Long rows: keys and the counts of their first digit, a workgroup for every kPartSlots slots, so that a few long rows are
+// gone through by many compute units.
+__global__ void __launch_bounds__(kPartThreads) k_evict_keys(EvictArgs a) {
+  __shared__ unsigned hist[kDigits];
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, first = blockIdx.x * kPartSlots;
+  const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
+  const int length = seq_length(a.seqs, b), total = a.total ? a.total[b] : length, stay = min(length, max(a.keep[b], 0));
+  if (first >= length || stay == 0 || stay == length) return;
+  for (int i = tid; i < kDigits; i += kPartThreads) hist[i] = 0;
+  __syncthreads();
+  constexpr int GROUP = 8, RUN = kPartSlots / (kPartThreads / kWave);
+  const int start = first + (tid >> 6) * RUN, end = min(length, start + RUN);
+  for (int s0 = start; s0 < end; s0 += GROUP * kWave) {
+    uint32_t key[GROUP];
+    keys_of<GROUP>(a, at, s0 + lane, length, total, key);
+#pragma unroll
+    for (int k = 0; k < GROUP; ++k) {
+      const int i = s0 + k * kWave + lane;
+      if (i < end) a.keys[row * a.seqs.max_len + i] = key[k];
+      count_digit(hist, i < end, key[k] >> (32 - kDigitBits), lane);
+    }
+  }
+  __syncthreads();
+  unsigned short* counts = a.digits + (row * a.parts + blockIdx.x) * kDigits;
+  for (int i = tid; i < kDigits; i += kPartThreads) counts[i] = (unsigned short)hist[i];
+}
+
+// One workgroup a (sequence, kv head); a wavefront has a run of slots, their keys in registers (KEYS a lane; 0: from the
+// workspace, which k_evict_keys has filled). The smallest key that stays is found by digits of ten bits, each counted in LDS, one thread a digit's count: the
+// first digit is the top one (sign, exponent, a bit of the weight); the keys that share it (a few hundred to a few thousand of
+// a long row) go on in a list in LDS, with ~number below the weight; every further digit starts at the highest bit in which
+// those left differ, so that equal weights or small numbers cost no rounds of their own. It ends when the digits so far cut
+// off exactly as many slots as stay. Then holes and movers are listed in the order of their slots, on ballots.
+template <int KEYS>
 __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
-  __shared__ unsigned hist[256];
-  __shared__ unsigned long long prefix_s;
-  __shared__ int left_s, done_s;
-  __shared__ int wave_holes[kEvictWaves], wave_movers[kEvictWaves];
+  constexpr bool READY = KEYS == 0;  // keys and the first digit's counts
+  constexpr int AHEAD = 8;
+  __shared__ unsigned hist[kDigits];
+  __shared__ unsigned long long list[kListMost];
+  __shared__ unsigned wave_a[kEvictWaves], wave_b[kEvictWaves], bits[4];  // bits: and, or of the keys that are left
+  __shared__ int digit_s, rest_s, count_s, listed_s;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
   const int length = seq_length(a.seqs, b), total = a.total ? a.total[b] : length;
   const int stay = min(length, max(a.keep[b], 0));
-  auto number = [&](int i) {
-    const int id = a.ids_in ? a.ids_in[at + i] : -1;
-    return id < 0 ? total - length + i : id;
+  const int its = (length + kEvictThreads - 1) / kEvictThreads, first = wave * its * kWave;  // its <= KEYS
+  const int steps = min(its, max(0, (length - first + kWave - 1) / kWave));                  // of this wavefront
+  const bool search = stay > 0 && stay < length;
+  const uint32_t* stored = a.keys + row * a.seqs.max_len;
+  uint32_t key[KEYS ? KEYS : 1];
+  if constexpr (KEYS != 0) {
+    if (search && steps > 0) keys_of<KEYS>(a, at, first + lane, length, total, key);
+  }
+  // f(slot of lane 0, this lane's slot, it is there, its key): every step of this wavefront
+  auto each = [&](auto f) {
+    int s0 = first, i = first + lane;
+    if constexpr (KEYS != 0) {
+#pragma unroll
+      for (int k = 0; k < KEYS; ++k) {
+        STTM_OPAQUE_V(i);  // (worked out where it is used: no register for every step's slot)
+        if (k < steps) f(s0, i, i < length, key[k]);
+        i += kWave;
+        s0 += kWave;
+      }
+    } else {
+      for (int k0 = 0; k0 < steps; k0 += AHEAD) {
+        uint32_t x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) x[k] = search ? stored[min(i + k * kWave, length - 1)] : 0u;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k, i += kWave, s0 += kWave)
+          if (k0 + k < steps) f(s0, i, i < length, x[k]);
+      }
+    }
   };
+  auto whole_key = [&](int i, uint32_t k) { return (unsigned long long)k << 32 | ~(uint32_t)slot_number(a, at, i, length, total); };
 
-  // Keys that agree with `prefix` in the bits above `shift` are still open; `left` of them stay.
+  // `prefix`: the digits so far, those to come zero; `left` of the keys that agree with it above `shift` stay.
   unsigned long long prefix = 0;
   int shift = 64, left = stay;
-  bool done = stay == length || stay == 0;
-  while (!done) {
-    shift -= 8;
-    for (int i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < length; i += kEvictThreads) {
-      const unsigned long long k = rank_key(a.weights_in[at + i], number(i), total, a);
-      if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
+  if (search) {
+    unsigned mine = 0;
+    if constexpr (READY) {
+      const unsigned short* counts = a.digits + row * a.parts * kDigits + tid;
+      const int parts = (length + kPartSlots - 1) / kPartSlots;
+#pragma unroll 8
+      for (int p = 0; p < parts; ++p) mine += counts[(long long)p * kDigits];
+      hist[tid] = mine;
+    } else {
+      hist[tid] = 0;
+      __syncthreads();
+      each([&](int, int, bool there, uint32_t k) { count_digit(hist, there, k >> (32 - kDigitBits), lane); });
     }
-    __syncthreads();
-    if (tid == 0) {
-      int rest = left, digit = 255;
-      while (digit > 0 && (int)hist[digit] < rest) rest -= (int)hist[digit--];
-      prefix_s = prefix | (unsigned long long)digit << shift;
-      left_s = rest;
-      done_s = (int)hist[digit] == rest || shift == 0;
+    if (tid == 0) listed_s = 0;
+    bool in_list = false;
+    int listed = 0;
+    shift = 64 - kDigitBits;
+    for (bool more = true; more;) {
+      __syncthreads();
+      // the digit at which the counts from the top reach `left`
+      const unsigned sum = hist[kDigits - 1 - tid];
+      unsigned upto = wave_inclusive(sum, lane);
+      if (lane == 63) wave_a[wave] = upto;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) upto += wave_a[w];
+      if (upto >= (unsigned)left && upto - sum < (unsigned)left) {  // one thread's
+        digit_s = kDigits - 1 - tid;
+        rest_s = left - (int)(upto - sum);
+        count_s = (int)sum;
+      }
+      if (tid < 4) bits[tid] = tid < 2 ? 0xffffffffu : 0u;
+      __syncthreads();
+      prefix |= (unsigned long long)digit_s << shift;
+      left = rest_s;
+      const int count = count_s;
+      if (left == count || shift == 0) break;
+      // those that are left: into the list once they fit it; the bits in which they differ
+      unsigned long long all = ~0ull, some = 0;
+      const bool gather = !in_list && count <= kListMost;
+      if (in_list) {
+        for (int i = tid; i < listed; i += kEvictThreads) {
+          const unsigned long long k = list[i];
+          if ((k >> shift) == (prefix >> shift)) { all &= k; some |= k; }
+        }
+      } else {
+        each([&](int, int i, bool there, uint32_t k) {
+          // (the number counts only where the weight alone does not tell)
+          const bool near = there && (shift >= 32 ? k >> (shift - 32) == (uint32_t)(prefix >> shift) : k == (uint32_t)(prefix >> 32));
+          if (__ballot(near) == 0) return;
+          if (near) {
+            const unsigned long long x = whole_key(i, k);
+            if ((x >> shift) == (prefix >> shift)) {
+              all &= x;
+              some |= x;
+              if (gather) list[atomicAdd(&listed_s, 1)] = x;
+            }
+          }
+        });
+      }
+      unsigned v[4] = {(unsigned)(all >> 32), (unsigned)all, (unsigned)(some >> 32), (unsigned)some};
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const unsigned y = __shfl_xor(v[x], o, 64);
+          v[x] = x < 2 ? v[x] & y : v[x] | y;
+        }
+      if (lane < 2) atomicAnd(&bits[lane], lane ? v[1] : v[0]);
+      else if (lane < 4) atomicOr(&bits[lane], lane == 3 ? v[3] : v[2]);
+      hist[tid] = 0;
+      __syncthreads();
+      if (gather) {
+        in_list = true;
+        listed = count;
+      }
+      const unsigned long long differ = ((unsigned long long)bits[0] << 32 | bits[1]) ^ ((unsigned long long)bits[2] << 32 | bits[3]);
+      const int above = shift;
+      if (differ == 0) {  // (the same number twice: any of them)
+        prefix |= ((unsigned long long)bits[0] << 32 | bits[1]) & ((1ull << above) - 1);
+        break;
+      }
+      shift = max(0, 64 - (int)__clzll((long long)differ) - kDigitBits);
+      // between the last digit and this one all agree
+      prefix |= ((unsigned long long)bits[0] << 32 | bits[1]) & ((1ull << above) - 1) & ~((1ull << shift) - 1) & ~((unsigned long long)(kDigits - 1) << shift);
+      // (the last digit of all may reach back into bits that are settled: both are compared)
+      const unsigned long long agree = prefix >> shift >> kDigitBits, settled = prefix >> above;
+      auto left_over = [&](unsigned long long k) { return (k >> shift >> kDigitBits) == agree && (k >> above) == settled; };
+      if (in_list) {
+        for (int i0 = 0; i0 < listed; i0 += kEvictThreads) {
+          const int i = i0 + tid;
+          const unsigned long long k = i < listed ? list[i] : 0;
+          count_digit(hist, i < listed && left_over(k), (uint32_t)(k >> shift) & (kDigits - 1), lane);
+        }
+      } else {
+        each([&](int, int i, bool there, uint32_t k) {
+          const bool near = there && (above >= 32 ? k >> (above - 32) == (uint32_t)(prefix >> above) : k == (uint32_t)(prefix >> 32));
+          const unsigned long long x = near ? whole_key(i, k) : 0;
+          count_digit(hist, near && left_over(x), (uint32_t)(x >> shift) & (kDigits - 1), lane);
+        });
+      }
     }
-    __syncthreads();
-    prefix = prefix_s;
-    left = left_s;
-    done = done_s != 0;
-    __syncthreads();
   }
-  // stays: key >= prefix (in the bits from `shift` up)
-  const bool all = stay == length, none = stay == 0;
+
+  const uint32_t least = (uint32_t)(prefix >> 32), least_low = (uint32_t)prefix;
+  // the slots of a step that stay / that there are / that lie before the new length, a bit each
+  auto staying = [&](int i, bool there, uint32_t k) {
+    if (!search) return __ballot(there && stay > 0);
+    bool yes = there && k >= least;
+    if (least_low != 0 && __ballot(yes && k == least) != 0 && yes && k == least)
+      yes = ~(uint32_t)slot_number(a, at, i, length, total) >= least_low;
+    return __ballot(yes);
+  };
+  auto up_to = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
   int holes = 0, movers = 0;
-  for (int i0 = 0; i0 < length; i0 += kEvictThreads) {
-    const int i = i0 + tid;
-    const bool in = i < length;
-    float w = 0.f, bias = 0.f;
-    int id = 0;
-    bool stays = false;
-    if (in) {
-      w = a.weights_in[at + i];
-      id = number(i);
-      if (a.bias_in) bias = a.bias_in[at + i];
-      stays = all || (!none && rank_key(w, id, total, a) >= prefix);
-    }
-    const bool hole = in && i < stay && !stays, mover = in && i >= stay && stays;
-    const unsigned long long hole_mask = __ballot(hole), mover_mask = __ballot(mover);
-    if (lane == 0) {
-      wave_holes[wave] = __popcll(hole_mask);
-      wave_movers[wave] = __popcll(mover_mask);
-    }
-    __syncthreads();
-    int my_hole = holes, my_mover = movers;
-    for (int v = 0; v < kEvictWaves; ++v) {
-      if (v < wave) { my_hole += wave_holes[v]; my_mover += wave_movers[v]; }
-      holes += wave_holes[v];
-      movers += wave_movers[v];
-    }
-    __syncthreads();
-    const unsigned long long below = (1ull << lane) - 1;
-    if (hole) a.holes[row * a.seqs.max_len + my_hole + __popcll(hole_mask & below)] = i;
-    if (mover) a.movers[row * a.seqs.max_len + my_mover + __popcll(mover_mask & below)] = Mover{i, id, w, bias};
-    if (in && !hole) {
-      const bool gone = i >= stay;
-      a.weights_out[at + i] = gone ? 0.f : w;
-      a.ids_out[at + i] = gone ? -1 : id;
-      if (a.bias_out) a.bias_out[at + i] = gone ? 0.f : bias;
-    }
+  each([&](int s0, int i, bool there, uint32_t k) {
+    const unsigned long long mask = staying(i, there, k), inside = up_to(length - s0), front = up_to(stay - s0);
+    holes += __popcll(~mask & inside & front);
+    movers += __popcll(mask & ~front);
+    if (lane == 0) a.stays[row * a.words + (s0 >> 6)] = mask;
+  });
+  __syncthreads();
+  if (lane == 0) {
+    wave_a[wave] = (unsigned)holes;
+    wave_b[wave] = (unsigned)movers;
   }
-  if (tid == 0) a.counts[row] = make_int2(movers, stay);
+  __syncthreads();
+  int my_hole = 0, my_mover = 0, all_holes = 0, all_movers = 0;
+  for (int w = 0; w < kEvictWaves; ++w) {
+    if (w < wave) {
+      my_hole += (int)wave_a[w];
+      my_mover += (int)wave_b[w];
+    }
+    all_holes += (int)wave_a[w];
+    all_movers += (int)wave_b[w];
+  }
+  const int pairs = min(min(all_holes, all_movers), a.pairs);  // (all three: as many of either, but for numbers that occur twice)
+  if (tid == 0) a.counts[row] = make_int4(pairs, stay, length, total);
+  if (pairs == 0) return;
+  const unsigned long long below = (1ull << lane) - 1;
+  int32_t *hole_list = a.holes + row * a.pairs, *mover_list = a.movers + row * a.pairs;
+  each([&](int s0, int i, bool there, uint32_t k) {
+    const unsigned long long mask = staying(i, there, k), inside = up_to(length - s0), front = up_to(stay - s0);
+    const unsigned long long hole = ~mask & inside & front, mover = mask & ~front;
+    if (hole) {
+      const int j = my_hole + __popcll(hole & below);
+      if ((hole >> lane & 1) && j < pairs) hole_list[j] = i;
+      my_hole += __popcll(hole);
+    }
+    if (mover) {
+      const int j = my_mover + __popcll(mover & below);
+      if ((mover >> lane & 1) && j < pairs) mover_list[j] = i;
+      my_mover += __popcll(mover);
+    }
+  });
 }
 
-// The j-th mover's rows go to the j-th hole: 2^LOG_LANES lanes a row, 16 bytes a lane.
-constexpr int kMoveThreads = 256;
+// The tables of the slots that neither move nor are filled, and the pairs: LANES lanes a row of the pool, 16 bytes a lane. A
+// mover's entries are read, written to its hole and cleared by one lane, nobody else touches either: outputs may be inputs.
+constexpr int kMoveThreads = 256, kMoveRows = 4;  // (rows of a group of lanes under way together)
 template <int LANES>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, unit = tid & (LANES - 1);
   const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
-  const int2 count = a.counts[row];
-  if (blockIdx.x == 0 && h == 0 && tid == 0) a.lengths_out[b] = count.y;
-  const int step = gridDim.x * (kMoveThreads / LANES), mask = (1 << a.pool.shift) - 1;
-  for (int j = blockIdx.x * (kMoveThreads / LANES) + tid / LANES; j < count.x; j += step) {
-    const Mover m = a.movers[row * a.seqs.max_len + j];
-    const int hole = a.holes[row * a.seqs.max_len + j];
-    if (unit == 0) {
-      a.weights_out[at + hole] = m.weight;
-      a.ids_out[at + hole] = m.id;
-      if (a.bias_out) a.bias_out[at + hole] = m.bias;
+  const int4 count = a.counts[row];
+  const int stay = count.y, length = count.z, total = count.w;
+  if (blockIdx.x == 0 && h == 0 && tid == 0) a.lengths_out[b] = stay;
+  for (int i = blockIdx.x * kMoveThreads + tid; i < length; i += gridDim.x * kMoveThreads) {
+    const bool stays = a.stays[row * a.words + (i >> 6)] >> (i & 63) & 1;
+    if (i >= stay) {
+      if (stays) continue;
+      a.weights_out[at + i] = 0.f;
+      a.ids_out[at + i] = -1;
+      if (a.bias_out) a.bias_out[at + i] = 0.f;
+    } else if (stays) {
+      a.weights_out[at + i] = a.weights_in[at + i];
+      a.ids_out[at + i] = slot_number(a, at, i, length, total);
+      if (a.bias_out) a.bias_out[at + i] = a.bias_in[at + i];
     }
-    const int p = a.seqs.table[b * a.seqs.table_stride + (m.slot >> a.pool.shift)];
-    const int q = a.seqs.table[b * a.seqs.table_stride + (hole >> a.pool.shift)];
-    if (p < 0 || p >= a.pool.pages || q < 0 || q >= a.pool.pages || unit * 16 >= a.pool.row) continue;
-    const long long from = p * a.pool.page_stride + h * a.pool.head_stride + (long long)(m.slot & mask) * a.pool.token_stride + unit * 16;
-    const long long to = q * a.pool.page_stride + h * a.pool.head_stride + (long long)(hole & mask) * a.pool.token_stride + unit * 16;
-    const uint4 k = *reinterpret_cast<const uint4*>(a.pool.k + from), v = *reinterpret_cast<const uint4*>(a.pool.v + from);
-    *reinterpret_cast<uint4*>(a.pool.k + to) = k;
-    *reinterpret_cast<uint4*>(a.pool.v + to) = v;
+  }
+  constexpr int GROUPS = kMoveThreads / LANES;
+  const int mask = (1 << a.pool.shift) - 1;
+  for (int j0 = blockIdx.x * GROUPS * kMoveRows + tid / LANES; j0 < count.x; j0 += gridDim.x * GROUPS * kMoveRows) {
+    int mover[kMoveRows], hole[kMoveRows], p[kMoveRows], q[kMoveRows];
+    uint4 k[kMoveRows], v[kMoveRows];
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      const int j = min(j0 + r * GROUPS, count.x - 1);
+      mover[r] = a.movers[row * a.pairs + j];
+      hole[r] = a.holes[row * a.pairs + j];
+    }
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      p[r] = a.seqs.table[b * a.seqs.table_stride + (mover[r] >> a.pool.shift)];
+      q[r] = a.seqs.table[b * a.seqs.table_stride + (hole[r] >> a.pool.shift)];
+      if (p[r] < 0 || p[r] >= a.pool.pages || q[r] < 0 || q[r] >= a.pool.pages || j0 + r * GROUPS >= count.x || unit * 16 >= a.pool.row) q[r] = -1;
+    }
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      if (q[r] < 0) continue;
+      const long long from = p[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(mover[r] & mask) * a.pool.token_stride + unit * 16;
+      k[r] = load_once(reinterpret_cast<const uint4*>(a.pool.k + from));
+      v[r] = load_once(reinterpret_cast<const uint4*>(a.pool.v + from));
+    }
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      if (unit != 0 || j0 + r * GROUPS >= count.x) continue;
+      const float w = a.weights_in[at + mover[r]];
+      const int id = slot_number(a, at, mover[r], length, total);
+      a.weights_out[at + hole[r]] = w;
+      a.ids_out[at + hole[r]] = id;
+      a.weights_out[at + mover[r]] = 0.f;
+      a.ids_out[at + mover[r]] = -1;
+      if (a.bias_out) {
+        const float bias = a.bias_in[at + mover[r]];
+        a.bias_out[at + hole[r]] = bias;
+        a.bias_out[at + mover[r]] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      if (q[r] < 0) continue;
+      const long long to = q[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(hole[r] & mask) * a.pool.token_stride + unit * 16;
+      store_once(reinterpret_cast<uint4*>(a.pool.k + to), k[r]);
+      store_once(reinterpret_cast<uint4*>(a.pool.v + to), v[r]);
+    }
   }
 }
 
 struct Plan {
-  size_t movers, holes, counts, bytes;
+  int words, pairs, parts;
+  size_t keys, digits, stays, holes, movers, counts, bytes;
 };
 Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   Plan p;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
   const size_t rows = (size_t)s->batch * c->kv_heads, slots = (size_t)make_seqs(c, s).max_len;
-  p.movers = take(rows * slots * sizeof(Mover));
-  p.holes = take(rows * slots * sizeof(int32_t));
-  p.counts = take(rows * sizeof(int2));
+  p.words = (int)((slots + 63) / 64);
+  p.pairs = (int)(slots / 2);
+  p.parts = slots > (size_t)kKeysHere * kEvictThreads ? (int)((slots + kPartSlots - 1) / kPartSlots) : 0;
+  p.keys = take(p.parts ? rows * slots * sizeof(uint32_t) : 0);
+  p.digits = take(rows * p.parts * kDigits * sizeof(unsigned short));
+  p.stays = take(rows * p.words * sizeof(unsigned long long));
+  p.holes = take(rows * p.pairs * sizeof(int32_t));
+  p.movers = take(rows * p.pairs * sizeof(int32_t));
+  p.counts = take(rows * sizeof(int4));
   p.bytes = std::max(off, (size_t)256);
   return p;
 }
@@ -214,17 +450,29 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   a.kv_heads = cache->kv_heads;
   a.sink = sink;
   a.recent = recent;
-  a.movers = reinterpret_cast<Mover*>(ws + p.movers);
+  a.keys = reinterpret_cast<uint32_t*>(ws + p.keys);
+  a.stays = reinterpret_cast<unsigned long long*>(ws + p.stays);
   a.holes = reinterpret_cast<int32_t*>(ws + p.holes);
-  a.counts = reinterpret_cast<int2*>(ws + p.counts);
+  a.movers = reinterpret_cast<int32_t*>(ws + p.movers);
+  a.counts = reinterpret_cast<int4*>(ws + p.counts);
+  a.digits = reinterpret_cast<unsigned short*>(ws + p.digits);
+  a.parts = p.parts;
+  a.words = p.words;
+  a.pairs = p.pairs;
   rc = ctx_device(ctx);
   if (rc != STTM_OK) return rc;
   const hipStream_t s = ctx_stream(ctx);
-  hipLaunchKernelGGL(k_evict_select, dim3(a.kv_heads, seqs->batch), dim3(kEvictThreads), 0, s, a);
+  const dim3 rows(a.kv_heads, seqs->batch), all(kEvictThreads);
+  if (p.parts) {
+    hipLaunchKernelGGL(k_evict_keys, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<0>), rows, all, 0, s, a);
+  } else {
+    hipLaunchKernelGGL((k_evict_select<kKeysHere>), rows, all, 0, s, a);
+  }
   const int lanes = a.pool.row <= 128 ? 8 : a.pool.row <= 256 ? 16 : a.pool.row <= 512 ? 32 : 64;
   // At most half of the slots move; some eight rows for a group of lanes.
   const int groups = kMoveThreads / lanes;
-  const dim3 grid(std::max(1, (a.seqs.max_len / 2 + 8 * groups - 1) / (8 * groups)), a.kv_heads, seqs->batch), block(kMoveThreads);
+  const dim3 grid(std::max(1, (p.pairs + 2 * kMoveRows * groups - 1) / (2 * kMoveRows * groups)), a.kv_heads, seqs->batch), block(kMoveThreads);
   if (lanes == 8) hipLaunchKernelGGL((k_evict_move<8>), grid, block, 0, s, a);
   else if (lanes == 16) hipLaunchKernelGGL((k_evict_move<16>), grid, block, 0, s, a);
   else if (lanes == 32) hipLaunchKernelGGL((k_evict_move<32>), grid, block, 0, s, a);

@@ -228,6 +228,9 @@ EVICT = [
     ("bf16", 2, 64, 64, (90, 70), (45, 1), 0, 1, "again", False, "odd", "slots"),        # NaN, infinities, both zeros
     ("f16", 2, 40, 8, (30,), (-4,), 0, 0, "none", True, "spread", "pages"),
     ("bf16", 1, 16, 8, (77,), (33,), 0, 0, "again", False, "equal", "pages"),
+    ("bf16", 2, 8, 64, (4097,), (4096,), 4, 64, "again", False, "zeros", "pages"),       # one goes, of many that are alike
+    ("f32", 1, 8, 64, (9001, 8193), (4500, 8192), 4, 64, "again", True, "zeros", "pages"),   # rows of several workgroups
+    ("bf16", 1, 8, 64, (8200, 33), (100, 5), 0, 0, "minus", False, "equal", "pages"),
 ]
 
 
@@ -243,6 +246,8 @@ def test_cache_evict(bench, case, alias):
         w = torch.randint(0, 3, (B, K, cap), generator=gen).float()
     if w_kind == "equal":
         w = torch.full((B, K, cap), 0.25)
+    if w_kind == "zeros":
+        w = torch.where(torch.rand(B, K, cap, generator=gen) < 0.1, 0.0, w)
     if w_kind == "odd":
         some = torch.tensor([math.nan, -math.nan, INF, -INF, 0.0, -0.0, 1e-42, -1.0])
         w = some[torch.randint(0, 8, (B, K, cap), generator=gen)]
@@ -264,6 +269,18 @@ def test_cache_evict(bench, case, alias):
             g = g.cpu()
             same = (g == x) | (torch.isnan(g) & torch.isnan(x)) if g.is_floating_point() else g == x
             assert same.all(), name
+
+
+def test_cache_evict_of_numbers_that_occur_twice(bench):
+    """Not allowed: which of them stay is open, but the lengths are as they have to be and nothing else is touched."""
+    gen = _gen(13)
+    n, keep = 300, 120
+    kv, table = C.pool(gen, "bf16", 1, 8, 8, (n,), junk=3.0)
+    w, ids = torch.zeros(1, 1, n), torch.full((1, 1, n), 7, dtype=torch.int32)
+    lens = torch.tensor([n], dtype=torch.int32)
+    outs = [torch.zeros_like(w), torch.zeros_like(ids), None]
+    got = C.run_evict(bench, kv, "pages", 8, table, lens, torch.tensor([keep], dtype=torch.int32), None, 0, 0, w, ids, None, *outs)
+    assert got[5].tolist() == [keep] and (got[3][0, 0, :keep] == 7).sum() <= keep
 
 
 def test_cache_evict_with_pages_outside_of_the_pool(bench):
