@@ -100,23 +100,20 @@ struct AttnArgs {
 // Softmax statistics of one head over several parts of the slots.
 __device__ inline float factor(float m, float top, float unit) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * unit); }
 
-// A slot's elements as one lane takes them: NV loads of 16 bytes (8 bytes: VW == 4 of 16 bits).
+// A slot's elements as one lane takes them: NV loads of 16 bytes (8 bytes: VW == 4 of 16 bits). A lane whose share lies
+// beyond the row takes the row's start in its place: what it makes of that is not written.
 template <int DT, int VW> struct ValueRow {
   static constexpr int WORDS = DT == 0 ? VW : VW / 2;
   uint32_t w[WORDS];
-  // `i`: lane % 16; bytes beyond the row are not read
-  __device__ inline void load(const char* row, int i, int bytes) {
+  __device__ inline void load(const char* row, int i, int bytes) {  // i: lane % 16
     if constexpr (DT != 0 && VW == 4) {
-      const int o = i * 8;
-      uint2 x = make_uint2(0u, 0u);
-      if (o < bytes) x = *reinterpret_cast<const uint2*>(row + o);
+      const uint2 x = *reinterpret_cast<const uint2*>(row + (i * 8 < bytes ? i * 8 : 0));
       w[0] = x.x; w[1] = x.y;
     } else {
 #pragma unroll
       for (int h = 0; h < WORDS / 4; ++h) {
         const int o = i * 16 + h * 256;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (o < bytes) x = *reinterpret_cast<const uint4*>(row + o);
+        const uint4 x = *reinterpret_cast<const uint4*>(row + (o < bytes ? o : 0));
         w[4 * h] = x.x; w[4 * h + 1] = x.y; w[4 * h + 2] = x.z; w[4 * h + 3] = x.w;
       }
     }
@@ -152,9 +149,16 @@ template <int DT> __device__ inline void store_channels(char* at, const float (&
 //
 // P is handed on as the sum of two 16-bit numbers (16 bits of mantissa with bf16, 22 with fp16), one product each: rounding it to
 // one alone would cost as much accuracy as the result's own rounding.
+//
+// Keys of the next block are loaded once this one's are used up, values likewise: no second set of registers, and there
+// are always some on their way. Two wavefronts a SIMD bound the registers to 256, which keeps the sums out of the
+// accumulation registers that only copies reach.
 template <int DT, int NQ, int VW, bool BIAS>
-__global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
+__global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attention(AttnArgs a) {
   constexpr int ES = DT == 0 ? 4 : 2, TILES = DT == 0 ? 1 : 2, BLOCK = 16 * TILES, PART = VW < 8 ? VW : 8;
+  constexpr int PIECES = DT == 0 ? NQ / 2 : NQ;  // (of 32 channels; the shortest row this instance is chosen for:)
+  constexpr int LEAST = ES * (PIECES <= 4 ? 32 * PIECES - 24 : PIECES == 6 ? 136 : 200);
+
   __shared__ long long page_at[kChunkMax / 8];        // byte offset of every page of the chunk, -1: not in the pool
   __shared__ float joined[kAttnWaves][PART * 4][kWave];  // the wavefronts' sums, a part of the channels at a time
   __shared__ float stat_m[kAttnWaves][kQTile], stat_l[kAttnWaves][kQTile];
@@ -164,7 +168,7 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
   const int first = chunk * a.chunk;
   if (first >= length && chunk > 0) return;  // (an empty sequence's first chunk is gone through: its result is written)
   const int end = min(length, first + a.chunk);
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, i16 = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g = lane >> 4;
   const int head0 = tile * kQTile, heads = min(kQTile, a.group - head0);
 
   for (int p = tid; p << a.pool.shift < end - first; p += kAttnThreads) {
@@ -195,11 +199,14 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
   const float* bias = BIAS ? a.bias + ((long long)b * a.kv_heads + h) * a.slot_stride : nullptr;
   float* logits = a.logits ? a.logits + ((long long)b * a.kv_heads + h) * a.seqs.max_len * a.group + head0 : nullptr;
 
-  for (int s0 = first + wave * BLOCK; s0 < end; s0 += kAttnWaves * BLOCK) {
-    // keys: lane i16 has the row of slot s0 + 16t + i16, its group's channels; values: slots s0 + 16t + 4g + r
-    u32x4 k[TILES][NQ];
-    ValueRow<DT, VW> v[TILES][4];
-    bool outside = false;
+  // keys: lane i16 has the row of slot s0 + 16t + i16, its group's channels; values: slots s0 + 16t + 4g + r. Slots from the
+  // end on are read as the last one. Loads stand without a branch around them: they are on their way together.
+  u32x4 k[TILES][NQ];
+  ValueRow<DT, VW> v[TILES][4];
+  bool outside = false, dead[TILES][4];
+  float add[TILES][4];
+  auto load_keys = [&](int s0) {
+    outside = false;
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       const int slot = min(s0 + 16 * t + i16, end - 1);
@@ -209,14 +216,14 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
 #pragma unroll
       for (int c = 0; c < NQ; ++c) {
         const int o = (c * 4 + g) * 16;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (at >= 0 && o < a.pool.row) x = *reinterpret_cast<const uint4*>(row + o);
+        const bool part = (c + 1) * 64 > LEAST;  // (the row may end in this piece)
+        const uint4 x = *reinterpret_cast<const uint4*>(row + (part && o >= a.pool.row ? 0 : o));
         k[t][c] = u32x4{x.x, x.y, x.z, x.w};
+        if (part && o >= a.pool.row) k[t][c] = u32x4{0u, 0u, 0u, 0u};
       }
     }
-    const bool careful = BIAS || s0 + BLOCK > end || __ballot(outside) != 0;  // (the same in all lanes: masked slots among these)
-    bool dead[TILES][4];
-    float add[TILES][4];
+  };
+  auto load_values = [&](int s0) {
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
@@ -227,6 +234,23 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         dead[t][r] = slot >= end || at < 0;
         v[t][r].load(a.pool.v + (at < 0 ? 0 : at) + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
       }
+  };
+  const int start = first + wave * BLOCK;
+  if (start < end) {
+    load_keys(start);
+    load_values(start);
+  }
+  for (int s0 = start; s0 < end; s0 += kAttnWaves * BLOCK) {
+    const bool careful = BIAS || s0 + BLOCK > end || __ballot(outside) != 0;  // (the same in all lanes: masked slots among these)
+    if (careful) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          dead[t][r] |= add[t][r] == -INFINITY;
+          if (dead[t][r]) v[t][r].clear();
+        }
+    }
     f32x4 s[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
@@ -241,15 +265,7 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         }
       }
     }
-    if (careful) {
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          dead[t][r] |= add[t][r] == -INFINITY;
-          if (dead[t][r]) v[t][r].clear();
-        }
-    }
+    load_keys(s0 + kAttnWaves * BLOCK);  // (the next block's, while this one goes on; past the end the last slot)
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
@@ -259,18 +275,26 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         if (careful && dead[t][r]) x = -INFINITY;
         s[t][r] = x;
         top = fmaxf(top, x);
-        if (logits && i16 < heads && s0 + 16 * t + 4 * g + r < end) logits[(long long)(s0 + 16 * t + 4 * g + r) * a.group + i16] = x;
       }
+    if (logits) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (i16 < heads && s0 + 16 * t + 4 * g + r < end) logits[(long long)(s0 + 16 * t + 4 * g + r) * a.group + i16] = s[t][r];
+    }
     top = fmaxf(top, __shfl_xor(top, 16, 64));
     top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float m2 = fmaxf(m, top), base = m2 == -INFINITY ? 0.f : m2;
-    const float shrink = exp2_fast((m - base) * a.unit);
-    m = m2;
-    l *= shrink;
+    if (__ballot(top > m) != 0) {  // (seldom after the first blocks)
+      const float m2 = fmaxf(m, top), shrink = factor(m, m2, a.unit);
+      m = m2;
+      l *= shrink;
 #pragma unroll
-    for (int n = 0; n < VW; ++n)
+      for (int n = 0; n < VW; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[n][r] *= shrink;
+        for (int r = 0; r < 4; ++r) acc[n][r] *= shrink;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
     float p[TILES][4];
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
@@ -304,6 +328,7 @@ __global__ void __launch_bounds__(kAttnThreads) k_paged_attention(AttnArgs a) {
         acc[n] = mma16<DT>(x, lo, acc[n]);
       }
     }
+    load_values(s0 + kAttnWaves * BLOCK);
   }
 
   // The wavefronts' sums on a common maximum, added up in their order.

@@ -17,7 +17,10 @@ struct EvictArgs {
   int32_t *ids_out, *lengths_out;
   int kv_heads, sink, recent;
   uint32_t* keys;              // [batch, kv_heads, max_len], of long rows, and
-  unsigned short* digits;      // [batch, kv_heads, parts, 1024]: counts of their top digits
+  unsigned short* digits;      // [batch, kv_heads, parts, 1024]: counts of their top digits,
+  int4* found;                 // [batch, kv_heads]: the digit the search goes on in, how many of it stay, how many share it,
+  uint2* list;                 // [batch, kv_heads, 4096]: those (key, slot), in any order,
+  int* listed;                 // [batch, kv_heads]: how many
   unsigned long long* stays;   // [batch, kv_heads, words]: a bit a slot
   int32_t *holes, *movers;     // [batch, kv_heads, pairs]: the j-th mover goes to the j-th hole
   int4* counts;                // [batch, kv_heads]: pairs, new length, length, tokens so far (seqs.lengths may be lengths_out)
@@ -80,10 +83,11 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_keys(EvictArgs a) {
   const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
   const int length = seq_length(a.seqs, b), total = a.total ? a.total[b] : length, stay = min(length, max(a.keep[b], 0));
   if (first >= length || stay == 0 || stay == length) return;
+  if (blockIdx.x == 0 && tid == 0) a.listed[row] = 0;
   for (int i = tid; i < kDigits; i += kPartThreads) hist[i] = 0;
   __syncthreads();
   constexpr int GROUP = 8, RUN = kPartSlots / (kPartThreads / kWave);
-  const int start = first + (tid >> 6) * RUN, end = min(length, start + RUN);
+  const int start = first + __builtin_amdgcn_readfirstlane(tid >> 6) * RUN, end = min(length, start + RUN);
   for (int s0 = start; s0 < end; s0 += GROUP * kWave) {
     uint32_t key[GROUP];
     keys_of<GROUP>(a, at, s0 + lane, length, total, key);
@@ -99,6 +103,81 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_keys(EvictArgs a) {
   for (int i = tid; i < kDigits; i += kPartThreads) counts[i] = (unsigned short)hist[i];
 }
 
+// Long rows, second pass: the digit at which the counts from the top reach the new length (every workgroup adds the parts up
+// for itself), a bit for every slot above it, and the slots that share it, as many as fit the list, for the search.
+__global__ void __launch_bounds__(kPartThreads) k_evict_mark(EvictArgs a) {
+  __shared__ unsigned wave_a[kPartThreads / kWave];
+  __shared__ int found[3];
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first = blockIdx.x * kPartSlots;
+  const long long row = (long long)b * a.kv_heads + h;
+  const int length = seq_length(a.seqs, b), stay = min(length, max(a.keep[b], 0));
+  if (first >= length) return;
+  const bool search = stay > 0 && stay < length;
+  int digit = 0, left = stay, count = length;
+  if (search) {
+    constexpr int PER = kDigits / kPartThreads;  // the digits of a thread, from the top
+    unsigned n[PER] = {}, sum = 0;
+    const unsigned short* counts = a.digits + row * a.parts * kDigits + kDigits - PER - tid * PER;
+    const int parts = (length + kPartSlots - 1) / kPartSlots;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+      const uint2 x = *reinterpret_cast<const uint2*>(counts + (long long)p * kDigits);
+      n[3] += x.x & 0xffffu; n[2] += x.x >> 16; n[1] += x.y & 0xffffu; n[0] += x.y >> 16;
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) sum += n[k];
+    unsigned upto = wave_inclusive(sum, lane);
+    if (lane == 63) wave_a[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += wave_a[w];
+    unsigned before = upto - sum;
+    if (before < (unsigned)stay && upto >= (unsigned)stay) {  // one thread's
+      bool open = true;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        if (open && before + n[k] >= (unsigned)stay) {
+          found[0] = kDigits - 1 - tid * PER - k;
+          found[1] = stay - (int)before;
+          found[2] = (int)n[k];
+          open = false;
+        }
+        before += n[k];
+      }
+    }
+    __syncthreads();
+    digit = found[0];
+    left = found[1];
+    count = found[2];
+  }
+  if (blockIdx.x == 0 && tid == 0) a.found[row] = make_int4(digit, left, count, 0);
+  const bool exact = !search || left == count, listed = !exact && count <= kListMost;
+  constexpr int GROUP = 8, RUN = kPartSlots / (kPartThreads / kWave);
+  const int start = first + wave * RUN, end = min(length, start + RUN);
+  const unsigned long long below = (1ull << lane) - 1;
+  uint2* list = a.list + row * kListMost;
+  for (int s0 = start; s0 < end; s0 += GROUP * kWave) {
+    uint32_t key[GROUP];
+#pragma unroll
+    for (int k = 0; k < GROUP; ++k) key[k] = search ? a.keys[row * a.seqs.max_len + min(s0 + k * kWave + lane, length - 1)] : 0u;
+#pragma unroll
+    for (int k = 0; k < GROUP; ++k) {
+      const int s = s0 + k * kWave, i = s + lane, d = (int)(key[k] >> (32 - kDigitBits));
+      if (s >= end) break;
+      const bool yes = i < end && (search ? d > digit || (exact && d == digit) : stay > 0);
+      const unsigned long long mask = __ballot(yes);
+      if (lane == 0) a.stays[row * a.words + (s >> 6)] = mask;
+      const unsigned long long near = __ballot(listed && i < end && d == digit);
+      if (near) {
+        int at = 0;
+        if (lane == 0) at = atomicAdd(a.listed + row, (int)__popcll(near));
+        at = lane_value(at, 0) + __popcll(near & below);
+        if ((near >> lane & 1) && at < kListMost) list[at] = make_uint2(key[k], (unsigned)i);
+      }
+    }
+  }
+}
+
 // One workgroup a (sequence, kv head); a wavefront has a run of slots, their keys in registers (KEYS a lane; 0: from the
 // workspace, which k_evict_keys has filled). The smallest key that stays is found by digits of ten bits, each counted in LDS, one thread a digit's count: the
 // first digit is the top one (sign, exponent, a bit of the weight); the keys that share it (a few hundred to a few thousand of
@@ -110,104 +189,118 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   constexpr bool READY = KEYS == 0;  // keys and the first digit's counts
   constexpr int AHEAD = 8;
   __shared__ unsigned hist[kDigits];
-  __shared__ unsigned long long list[kListMost];
+  __shared__ unsigned long long list[kListMost], word_s[kEvictThreads];
+  __shared__ unsigned list_slot[READY ? kListMost : 1];
+  __shared__ int2 base_s[kEvictThreads];
   __shared__ unsigned wave_a[kEvictWaves], wave_b[kEvictWaves], bits[4];  // bits: and, or of the keys that are left
   __shared__ int digit_s, rest_s, count_s, listed_s;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
   const int length = seq_length(a.seqs, b), total = a.total ? a.total[b] : length;
   const int stay = min(length, max(a.keep[b], 0));
   const int its = (length + kEvictThreads - 1) / kEvictThreads, first = wave * its * kWave;  // its <= KEYS
   const int steps = min(its, max(0, (length - first + kWave - 1) / kWave));                  // of this wavefront
   const bool search = stay > 0 && stay < length;
+  const unsigned long long below = (1ull << lane) - 1;
   const uint32_t* stored = a.keys + row * a.seqs.max_len;
   uint32_t key[KEYS ? KEYS : 1];
   if constexpr (KEYS != 0) {
     if (search && steps > 0) keys_of<KEYS>(a, at, first + lane, length, total, key);
   }
-  // f(slot of lane 0, this lane's slot, it is there, its key): every step of this wavefront
-  auto each = [&](auto f) {
+  // f(slot of lane 0, this lane's slot, it is there, its key, its token's number if `numbers`): every step of this wavefront
+  auto each = [&](bool numbers, auto f) {
     int s0 = first, i = first + lane;
-    if constexpr (KEYS != 0) {
+    for (int k0 = 0; k0 < steps; k0 += AHEAD) {
+      uint32_t x[AHEAD];
+      int id[AHEAD];
 #pragma unroll
-      for (int k = 0; k < KEYS; ++k) {
-        STTM_OPAQUE_V(i);  // (worked out where it is used: no register for every step's slot)
-        if (k < steps) f(s0, i, i < length, key[k]);
-        i += kWave;
-        s0 += kWave;
+      for (int k = 0; k < AHEAD; ++k) {
+        const int at_slot = min(i + k * kWave, length - 1);
+        if constexpr (KEYS != 0) x[k] = key[k];  // (one round)
+        else x[k] = search ? stored[at_slot] : 0u;
+        id[k] = numbers && a.ids_in ? a.ids_in[at + at_slot] : -1;
       }
-    } else {
-      for (int k0 = 0; k0 < steps; k0 += AHEAD) {
-        uint32_t x[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) x[k] = search ? stored[min(i + k * kWave, length - 1)] : 0u;
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k, i += kWave, s0 += kWave)
-          if (k0 + k < steps) f(s0, i, i < length, x[k]);
-      }
+      for (int k = 0; k < AHEAD; ++k, i += kWave, s0 += kWave)
+        if (k0 + k < steps) f(s0, i, i < length, x[k], id[k] < 0 ? total - length + i : id[k]);
     }
   };
-  auto whole_key = [&](int i, uint32_t k) { return (unsigned long long)k << 32 | ~(uint32_t)slot_number(a, at, i, length, total); };
+  auto whole_key = [](uint32_t k, int id) { return (unsigned long long)k << 32 | ~(uint32_t)id; };
 
   // `prefix`: the digits so far, those to come zero; `left` of the keys that agree with it above `shift` stay.
   unsigned long long prefix = 0;
-  int shift = 64, left = stay;
+  int shift = 64 - kDigitBits, left = stay;
+  bool in_list = false, marked = false;  // marked: the bits of all slots but those in the list are there
+  int listed = 0;
   if (search) {
-    unsigned mine = 0;
+    if (tid == 0) listed_s = 0;
     if constexpr (READY) {
-      const unsigned short* counts = a.digits + row * a.parts * kDigits + tid;
-      const int parts = (length + kPartSlots - 1) / kPartSlots;
-#pragma unroll 8
-      for (int p = 0; p < parts; ++p) mine += counts[(long long)p * kDigits];
-      hist[tid] = mine;
+      const int4 found = a.found[row];
+      prefix = (unsigned long long)found.x << shift;
+      left = found.y;
+      marked = left == found.z || found.z <= kListMost;
+      if (left != found.z && marked) {
+        listed = found.z;
+        in_list = true;
+        for (int i = tid; i < listed; i += kEvictThreads) {
+          const uint2 x = a.list[row * kListMost + i];
+          list[i] = whole_key(x.x, slot_number(a, at, (int)x.y, length, total));
+          list_slot[i] = x.y;
+        }
+      }
+      if (tid == 0) count_s = found.z;
     } else {
       hist[tid] = 0;
       __syncthreads();
-      each([&](int, int, bool there, uint32_t k) { count_digit(hist, there, k >> (32 - kDigitBits), lane); });
+      each(false, [&](int, int, bool there, uint32_t k, int) { count_digit(hist, there, k >> (32 - kDigitBits), lane); });
     }
-    if (tid == 0) listed_s = 0;
-    bool in_list = false;
-    int listed = 0;
-    shift = 64 - kDigitBits;
+    bool picked = READY;  // (the first digit)
     for (bool more = true; more;) {
       __syncthreads();
-      // the digit at which the counts from the top reach `left`
-      const unsigned sum = hist[kDigits - 1 - tid];
-      unsigned upto = wave_inclusive(sum, lane);
-      if (lane == 63) wave_a[wave] = upto;
-      __syncthreads();
-      for (int w = 0; w < wave; ++w) upto += wave_a[w];
-      if (upto >= (unsigned)left && upto - sum < (unsigned)left) {  // one thread's
-        digit_s = kDigits - 1 - tid;
-        rest_s = left - (int)(upto - sum);
-        count_s = (int)sum;
+      if (!picked) {
+        // the digit at which the counts from the top reach `left`
+        const unsigned sum = hist[kDigits - 1 - tid];
+        unsigned upto = wave_inclusive(sum, lane);
+        if (lane == 63) wave_a[wave] = upto;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) upto += wave_a[w];
+        if (upto >= (unsigned)left && upto - sum < (unsigned)left) {  // one thread's
+          digit_s = kDigits - 1 - tid;
+          rest_s = left - (int)(upto - sum);
+          count_s = (int)sum;
+        }
+        __syncthreads();
+        prefix |= (unsigned long long)digit_s << shift;
+        left = rest_s;
       }
+      picked = false;
+      const int count = count_s;
       if (tid < 4) bits[tid] = tid < 2 ? 0xffffffffu : 0u;
       __syncthreads();
-      prefix |= (unsigned long long)digit_s << shift;
-      left = rest_s;
-      const int count = count_s;
       if (left == count || shift == 0) break;
       // those that are left: into the list once they fit it; the bits in which they differ
       unsigned long long all = ~0ull, some = 0;
-      const bool gather = !in_list && count <= kListMost;
+      const bool gather = !READY && !in_list && count <= kListMost;
       if (in_list) {
         for (int i = tid; i < listed; i += kEvictThreads) {
           const unsigned long long k = list[i];
           if ((k >> shift) == (prefix >> shift)) { all &= k; some |= k; }
         }
       } else {
-        each([&](int, int i, bool there, uint32_t k) {
-          // (the number counts only where the weight alone does not tell)
-          const bool near = there && (shift >= 32 ? k >> (shift - 32) == (uint32_t)(prefix >> shift) : k == (uint32_t)(prefix >> 32));
-          if (__ballot(near) == 0) return;
+        each(true, [&](int, int, bool there, uint32_t k, int id) {
+          const unsigned long long x = whole_key(k, id);
+          const bool near = there && (x >> shift) == (prefix >> shift);
+          const unsigned long long mask = __ballot(near);
+          if (mask == 0) return;
           if (near) {
-            const unsigned long long x = whole_key(i, k);
-            if ((x >> shift) == (prefix >> shift)) {
-              all &= x;
-              some |= x;
-              if (gather) list[atomicAdd(&listed_s, 1)] = x;
-            }
+            all &= x;
+            some |= x;
+          }
+          if (gather) {
+            int base = 0;
+            if (lane == 0) base = atomicAdd(&listed_s, (int)__popcll(mask));
+            base = lane_value(base, 0);
+            if (near) list[base + __popcll(mask & below)] = x;
           }
         });
       }
@@ -246,66 +339,80 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
           count_digit(hist, i < listed && left_over(k), (uint32_t)(k >> shift) & (kDigits - 1), lane);
         }
       } else {
-        each([&](int, int i, bool there, uint32_t k) {
-          const bool near = there && (above >= 32 ? k >> (above - 32) == (uint32_t)(prefix >> above) : k == (uint32_t)(prefix >> 32));
-          const unsigned long long x = near ? whole_key(i, k) : 0;
-          count_digit(hist, near && left_over(x), (uint32_t)(x >> shift) & (kDigits - 1), lane);
+        each(true, [&](int, int, bool there, uint32_t k, int id) {
+          const unsigned long long x = whole_key(k, id);
+          count_digit(hist, there && left_over(x), (uint32_t)(x >> shift) & (kDigits - 1), lane);
         });
       }
     }
   }
 
-  const uint32_t least = (uint32_t)(prefix >> 32), least_low = (uint32_t)prefix;
-  // the slots of a step that stay / that there are / that lie before the new length, a bit each
-  auto staying = [&](int i, bool there, uint32_t k) {
-    if (!search) return __ballot(there && stay > 0);
-    bool yes = there && k >= least;
-    if (least_low != 0 && __ballot(yes && k == least) != 0 && yes && k == least)
-      yes = ~(uint32_t)slot_number(a, at, i, length, total) >= least_low;
-    return __ballot(yes);
-  };
+  // a bit for every slot that stays
+  if (!READY || !marked) {
+    const uint32_t least = (uint32_t)(prefix >> 32), least_low = (uint32_t)prefix;
+    if (!READY || search)
+      each(search && least_low != 0, [&](int s0, int, bool there, uint32_t k, int id) {
+        const unsigned long long mask = __ballot(there && (search ? k > least || (k == least && ~(uint32_t)id >= least_low) : stay > 0));
+        if (lane == 0) a.stays[row * a.words + (s0 >> 6)] = mask;
+      });
+  }
+  // Holes and movers, a round of words at a time: a thread counts a word's, then a wavefront lists a word's.
+  const int words = (length + 63) / 64;
   auto up_to = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
   int holes = 0, movers = 0;
-  each([&](int s0, int i, bool there, uint32_t k) {
-    const unsigned long long mask = staying(i, there, k), inside = up_to(length - s0), front = up_to(stay - s0);
-    holes += __popcll(~mask & inside & front);
-    movers += __popcll(mask & ~front);
-    if (lane == 0) a.stays[row * a.words + (s0 >> 6)] = mask;
-  });
-  __syncthreads();
-  if (lane == 0) {
-    wave_a[wave] = (unsigned)holes;
-    wave_b[wave] = (unsigned)movers;
+  for (int w0 = 0; w0 < words; w0 += kEvictThreads) {
+    __syncthreads();
+    const int word = w0 + tid, s0 = word * 64;
+    if (word < words) word_s[tid] = a.stays[row * a.words + word];
+    __syncthreads();
+    if (in_list && marked) {
+      unsigned* half = reinterpret_cast<unsigned*>(word_s);
+      for (int i = tid; i < listed; i += kEvictThreads) {
+        const int at_word = (int)(list_slot[i] >> 6) - w0;
+        if (list[i] >= prefix && at_word >= 0 && at_word < kEvictThreads) atomicOr(&half[2 * at_word + (list_slot[i] >> 5 & 1)], 1u << (list_slot[i] & 31));
+      }
+      __syncthreads();
+      if (word < words) a.stays[row * a.words + word] = word_s[tid];
+    }
+    unsigned long long hole = 0, mover = 0;
+    if (word < words) {
+      const unsigned long long mask = word_s[tid], front = up_to(stay - s0);
+      hole = ~mask & up_to(length - s0) & front;
+      mover = mask & ~front;
+    }
+    unsigned my_hole = (unsigned)__popcll(hole), my_mover = (unsigned)__popcll(mover);
+    const unsigned own_hole = my_hole, own_mover = my_mover;
+    my_hole = wave_inclusive(my_hole, lane);
+    my_mover = wave_inclusive(my_mover, lane);
+    if (lane == 63) {
+      wave_a[wave] = my_hole;
+      wave_b[wave] = my_mover;
+    }
+    __syncthreads();
+    int round_holes = 0, round_movers = 0;
+    for (int w = 0; w < kEvictWaves; ++w) {
+      if (w == wave) {
+        base_s[tid] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
+      }
+      round_holes += (int)wave_a[w];
+      round_movers += (int)wave_b[w];
+    }
+    __syncthreads();
+    const unsigned long long below = (1ull << lane) - 1;
+    for (int w = wave; w < min(kEvictThreads, words - w0); w += kEvictWaves) {
+      const int slot0 = (w0 + w) * 64;
+      const unsigned long long mask = word_s[w], front = up_to(stay - slot0);
+      const unsigned long long hole_mask = ~mask & up_to(length - slot0) & front, mover_mask = mask & ~front;
+      const int2 base = base_s[w];
+      const int i = base.x + __popcll(hole_mask & below), j = base.y + __popcll(mover_mask & below);
+      if ((hole_mask >> lane & 1) && i < a.pairs) a.holes[row * a.pairs + i] = slot0 + lane;
+      if ((mover_mask >> lane & 1) && j < a.pairs) a.movers[row * a.pairs + j] = slot0 + lane;
+    }
+    holes += round_holes;
+    movers += round_movers;
   }
-  __syncthreads();
-  int my_hole = 0, my_mover = 0, all_holes = 0, all_movers = 0;
-  for (int w = 0; w < kEvictWaves; ++w) {
-    if (w < wave) {
-      my_hole += (int)wave_a[w];
-      my_mover += (int)wave_b[w];
-    }
-    all_holes += (int)wave_a[w];
-    all_movers += (int)wave_b[w];
-  }
-  const int pairs = min(min(all_holes, all_movers), a.pairs);  // (all three: as many of either, but for numbers that occur twice)
-  if (tid == 0) a.counts[row] = make_int4(pairs, stay, length, total);
-  if (pairs == 0) return;
-  const unsigned long long below = (1ull << lane) - 1;
-  int32_t *hole_list = a.holes + row * a.pairs, *mover_list = a.movers + row * a.pairs;
-  each([&](int s0, int i, bool there, uint32_t k) {
-    const unsigned long long mask = staying(i, there, k), inside = up_to(length - s0), front = up_to(stay - s0);
-    const unsigned long long hole = ~mask & inside & front, mover = mask & ~front;
-    if (hole) {
-      const int j = my_hole + __popcll(hole & below);
-      if ((hole >> lane & 1) && j < pairs) hole_list[j] = i;
-      my_hole += __popcll(hole);
-    }
-    if (mover) {
-      const int j = my_mover + __popcll(mover & below);
-      if ((mover >> lane & 1) && j < pairs) mover_list[j] = i;
-      my_mover += __popcll(mover);
-    }
-  });
+  // (all three alike, and as many as there is room for, but for numbers that occur twice)
+  if (tid == 0) a.counts[row] = make_int4(min(min(holes, movers), a.pairs), stay, length, total);
 }
 
 // The tables of the slots that neither move nor are filled, and the pairs: LANES lanes a row of the pool, 16 bytes a lane. A
@@ -382,7 +489,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
 
 struct Plan {
   int words, pairs, parts;
-  size_t keys, digits, stays, holes, movers, counts, bytes;
+  size_t keys, digits, found, list, listed, stays, holes, movers, counts, bytes;
 };
 Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   Plan p;
@@ -394,6 +501,9 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   p.parts = slots > (size_t)kKeysHere * kEvictThreads ? (int)((slots + kPartSlots - 1) / kPartSlots) : 0;
   p.keys = take(p.parts ? rows * slots * sizeof(uint32_t) : 0);
   p.digits = take(rows * p.parts * kDigits * sizeof(unsigned short));
+  p.found = take(p.parts ? rows * sizeof(int4) : 0);
+  p.list = take(p.parts ? rows * kListMost * sizeof(uint2) : 0);
+  p.listed = take(p.parts ? rows * sizeof(int) : 0);
   p.stays = take(rows * p.words * sizeof(unsigned long long));
   p.holes = take(rows * p.pairs * sizeof(int32_t));
   p.movers = take(rows * p.pairs * sizeof(int32_t));
@@ -456,6 +566,9 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   a.movers = reinterpret_cast<int32_t*>(ws + p.movers);
   a.counts = reinterpret_cast<int4*>(ws + p.counts);
   a.digits = reinterpret_cast<unsigned short*>(ws + p.digits);
+  a.found = reinterpret_cast<int4*>(ws + p.found);
+  a.list = reinterpret_cast<uint2*>(ws + p.list);
+  a.listed = reinterpret_cast<int*>(ws + p.listed);
   a.parts = p.parts;
   a.words = p.words;
   a.pairs = p.pairs;
@@ -465,6 +578,7 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   const dim3 rows(a.kv_heads, seqs->batch), all(kEvictThreads);
   if (p.parts) {
     hipLaunchKernelGGL(k_evict_keys, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
+    hipLaunchKernelGGL(k_evict_mark, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
     hipLaunchKernelGGL((k_evict_select<0>), rows, all, 0, s, a);
   } else {
     hipLaunchKernelGGL((k_evict_select<kKeysHere>), rows, all, 0, s, a);

@@ -127,7 +127,7 @@ constexpr int kRopeThreads = 256;
 template <int DT, int LANES>
 __global__ void __launch_bounds__(kRopeThreads) k_qk_norm_rope(RopeArgs a) {
   constexpr int ES = DT == 0 ? 4 : 2, ROWS = kWave / LANES;
-  const long long wave = (long long)blockIdx.x * (kRopeThreads / kWave) + (threadIdx.x >> 6);
+  const long long wave = (long long)blockIdx.x * (kRopeThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long row = wave / a.parts;
   if (row >= a.n) return;  // (the same in all lanes)
   const int part = (int)(wave % a.parts), lane = threadIdx.x & 63, unit = lane & (LANES - 1), sub = lane / LANES;
