@@ -152,11 +152,12 @@ class PagedCache:
                 "k and v must be [pages, kv_heads, page_size, head_dim] with the same strides, the last one 1")
         _expect(k.dtype == v.dtype and k.dtype in _DTYPES, STTM_ERR_DTYPE, "k and v must be of one type, float32, bfloat16 or float16")
         _expect(k.device == v.device, STTM_ERR_ARG, "k and v must be on one device")
-        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.get_device()   # (the tensors live as long as this)
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         strides = [st if n > 1 else 0 for n, st in zip(k.shape, k.stride())]   # (the stride of a single entry means nothing)
         self.struct = _CacheStruct(_ptr(k), _ptr(v), _DTYPES[k.dtype], self.kv_heads, self.head_dim, self.page_size, self.pages,
                                    strides[0], strides[1], strides[2] or self.head_dim)
+        self.ref = C.byref(self.struct)
 
 
 class Sequences:
@@ -172,10 +173,11 @@ class Sequences:
                 "the rows of block_table and lengths must be contiguous")
         _expect(block_table.device == lengths.device, STTM_ERR_ARG, "block_table and lengths must be on one device")
         _expect(max_len is None or max_len >= 0, STTM_ERR_SHAPE, "max_len must not be negative")
-        self.block_table, self.lengths, self.batch, self.device = block_table, lengths, batch, lengths.device
+        self.block_table, self.lengths, self.batch, self.device = block_table, lengths, batch, lengths.get_device()
         self.max_pages, self.max_len = pages, 2**31 - 1 if max_len is None else min(int(max_len), 2**31 - 1)
         self.struct = _SequencesStruct(_ptr(block_table), _ptr(lengths), block_table.stride(0) if batch > 1 else pages, batch, pages,
                                        self.max_len)
+        self.ref = C.byref(self.struct)
 
 
 class Rope:
@@ -194,10 +196,11 @@ class Rope:
         _expect(1 <= len(parts) <= min(3, max(1, positions.shape[1])) and sum(parts) == inv_freq.numel() and min(parts) >= 0, STTM_ERR_SHAPE,
                 "sections: one to three numbers of pairs that add up to inv_freq's, no more of them than positions has axes")
         _expect(positions.device == inv_freq.device, STTM_ERR_ARG, "positions and inv_freq must be on one device")
-        self.positions, self.inv_freq, self.device, self.n = positions, inv_freq, inv_freq.device, positions.shape[0]
+        self.positions, self.inv_freq, self.device, self.n = positions, inv_freq, inv_freq.get_device(), positions.shape[0]
         stride = positions.stride(0) if self.n > 1 else positions.shape[1]
         self.struct = _RopeStruct(_ptr(positions), _ptr(inv_freq), stride, (C.c_int * 3)(*parts, *[0] * (3 - len(parts))),
                                   int(positions.dtype == torch.float32), int(interleaved))
+        self.ref = C.byref(self.struct)
 
 
 def sttm_paged_attention_workspace_bytes(cache: PagedCache, sequences: Sequences, q_heads: int, weights: bool = False) -> int:
@@ -208,34 +211,38 @@ def sttm_cache_evict_workspace_bytes(cache: PagedCache, sequences: Sequences) ->
     return int(_lib.sttm_cache_evict_workspace_bytes(cache.struct, sequences.struct))
 
 
-def _row_stride(t, name: str, n: int, like) -> int:
+# The checks below run on every call of a decoding loop: a handful of comparisons, messages only where one fails.
+
+def _rows(t, name: str, n: int, heads: int, d: int, dtype, device: int) -> int:
     """The elements between the rows of t [n, heads, d], whose heads lie one after the other."""
-    shape, stride = t.shape, t.stride()
-    heads = shape[1] if len(shape) == 3 else 0
-    if (len(shape) != 3 or shape[0] != n or (heads > 1 and stride[1] != shape[2]) or (stride[2] != 1 and shape[2] > 1)):
-        raise SttmError(STTM_ERR_SHAPE, f"{name} must be [{n}, heads, head_dim], the heads of a row one after the other")
-    if t.dtype != like.dtype or t.device != like.device:
+    stride = t.stride()
+    if t.shape != (n, heads, d) or stride[2] != 1 or (stride[1] != d and heads != 1):
+        raise SttmError(STTM_ERR_SHAPE, f"{name} must be [{n}, {heads}, {d}], the heads of a row one after the other")
+    if t.dtype is not dtype or t.get_device() != device:
         raise SttmError(STTM_ERR_DTYPE, f"{name} must be of the type and on the device of the others")
-    return stride[0] if n > 1 else heads * shape[2]
+    return stride[0] if n > 1 else heads * d
 
 
-def _slot_table(t, name: str, dtype, shape, device):
-    """t [batch, kv_heads, slots], rows contiguous and evenly apart."""
+def _table(t, name: str, dtype, shape, device: int) -> Optional[int]:
+    """The address of t [batch, kv_heads, slots], contiguous, or None."""
     if t is None:
-        return
-    if t.dtype != dtype or t.device != device:
+        return None
+    if t.dtype is not dtype or t.get_device() != device:
         raise SttmError(STTM_ERR_DTYPE, f"{name} must be {dtype} on the cache's device")
     if t.shape != shape or not t.is_contiguous():
         raise SttmError(STTM_ERR_SHAPE, f"{name} must be [batch, kv_heads, slots], contiguous, with as many slots as the other tables")
+    return t.data_ptr()
 
 
-def _vector(t, name: str, dtype, n: int, device):
+def _vector(t, name: str, dtype, n: int, device: int) -> Optional[int]:
+    """The address of t, n entries, or None."""
     if t is None:
-        return
-    if t.dtype != dtype or t.device != device:
+        return None
+    if t.dtype is not dtype or t.get_device() != device:
         raise SttmError(STTM_ERR_DTYPE, f"{name} must be {dtype} on the device of the others")
     if t.numel() != n or not t.is_contiguous():
         raise SttmError(STTM_ERR_SHAPE, f"{name} must have {n} entries, contiguous")
+    return t.data_ptr()
 
 
 def _ptr(t) -> Optional[int]:
@@ -260,7 +267,7 @@ class Sttm:
         rc = _lib.sttm_create(C.byref(self._h), device, C.c_void_p(stream_ptr))
         if rc != STTM_OK:
             raise SttmError(rc, "sttm_create failed")
-        self.device = device
+        self.device = self._device_index = device
         self._ws = None
         self.shape = None
 
@@ -351,88 +358,92 @@ class Sttm:
                                         _ptr(survived), _ptr(reassigned), _ptr(merged_pos), _ptr(root_tyxl)))
 
     # -- the reduced sequence in a model: a paged cache of keys and values -----------------------------
-    def _on_device(self, t):
-        if t.device.index != self.device:
+    def _on_device(self, device: int):
+        if device != self._device_index:
             raise SttmError(STTM_ERR_ARG, "the tensors must be on the context's device")
+
+    def _scratch(self, t, device: int):
+        if t is None:
+            return None, 0
+        if t.get_device() != device:
+            raise SttmError(STTM_ERR_ARG, "the workspace must be on the tensors' device")
+        if not t.is_contiguous():
+            raise SttmError(STTM_ERR_SHAPE, "the workspace must be contiguous")
+        return t.data_ptr(), t.nbytes
 
     def sttm_qk_norm_rope(self, q, k, v, q_out, k_out=None, cache: Optional[PagedCache] = None, slots=None, q_weight=None,
                           k_weight=None, eps: float = 1e-6, rope: Optional[Rope] = None):
         """q [n, q_heads, d], k and v [n, kv_heads, d] (views of one projection's output will do); q_out, k_out of the same
         shapes (or q and k themselves). cache, slots int64 [n]: where keys and values go."""
-        self._on_device(q)
-        n, q_heads, d = q.shape if q.dim() == 3 else (-1, 0, 0)
-        qs, ks, qos = _row_stride(q, "q", n, q), _row_stride(k, "k", n, q), _row_stride(q_out, "q_out", n, q)
-        kv_heads = k.shape[1]
-        if k.shape[2] != d or q_out.shape[1:] != (q_heads, d):
-            raise SttmError(STTM_ERR_SHAPE, "k must have q's head_dim, q_out q's shape")
-        vs = kos = 0
-        if k_out is not None:
-            kos = _row_stride(k_out, "k_out", n, q)
-            if k_out.shape[1:] != (kv_heads, d):
-                raise SttmError(STTM_ERR_SHAPE, "k_out must have k's shape")
-        if cache is not None:
-            vs = _row_stride(v, "v", n, q)
-            if v.shape[1:] != (kv_heads, d):
-                raise SttmError(STTM_ERR_SHAPE, "v must have k's shape")
-            if slots is None or cache.device != q.device:
-                raise SttmError(STTM_ERR_ARG, "a cache on the same device, and the rows' slots in it")
-            _vector(slots, "slots", torch.int64, n, q.device)
-        if rope is not None and (rope.n != n or rope.device != q.device):
-            raise SttmError(STTM_ERR_SHAPE, "the rotation must have a position for each row, on the same device")
-        _vector(q_weight, "q_weight", q.dtype, d, q.device)
-        _vector(k_weight, "k_weight", q.dtype, d, q.device)
-        if q.dtype not in _DTYPES:
+        if q.dim() != 3 or k.dim() != 3:
+            raise SttmError(STTM_ERR_SHAPE, "q and k must be [n, heads, head_dim]")
+        n, q_heads, d = q.shape
+        kv_heads, dtype, dev = k.shape[1], q.dtype, q.get_device()
+        self._on_device(dev)
+        if dtype not in _DTYPES:
             raise SttmError(STTM_ERR_DTYPE, "float32, bfloat16 or float16")
-        self._check(_lib.sttm_qk_norm_rope(self._h, _DTYPES[q.dtype], n, q_heads, kv_heads, d, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs,
-                                           _ptr(q_weight), _ptr(k_weight), eps, rope.struct if rope is not None else None,
-                                           _ptr(q_out), qos, _ptr(k_out), kos, cache.struct if cache is not None else None, _ptr(slots)))
+        qs, ks = _rows(q, "q", n, q_heads, d, dtype, dev), _rows(k, "k", n, kv_heads, d, dtype, dev)
+        qos = _rows(q_out, "q_out", n, q_heads, d, dtype, dev)
+        vs = kos = 0
+        v_at = k_out_at = slots_at = None
+        if k_out is not None:
+            kos, k_out_at = _rows(k_out, "k_out", n, kv_heads, d, dtype, dev), k_out.data_ptr()
+        if cache is not None:
+            if slots is None or v is None or cache.device != dev:
+                raise SttmError(STTM_ERR_ARG, "a cache on the same device, values, and the rows' slots in it")
+            vs, v_at = _rows(v, "v", n, kv_heads, d, dtype, dev), v.data_ptr()
+            slots_at = _vector(slots, "slots", torch.int64, n, dev)
+        if rope is not None and (rope.n != n or rope.device != dev):
+            raise SttmError(STTM_ERR_SHAPE, "the rotation must have a position for each row, on the same device")
+        rc = _lib.sttm_qk_norm_rope(self._h, _DTYPES[dtype], n, q_heads, kv_heads, d, q.data_ptr(), qs, k.data_ptr(), ks, v_at, vs,
+                                    _vector(q_weight, "q_weight", dtype, d, dev), _vector(k_weight, "k_weight", dtype, d, dev), eps,
+                                    rope.ref if rope is not None else None, q_out.data_ptr(), qos, k_out_at, kos,
+                                    cache.ref if cache is not None else None, slots_at)
+        if rc != STTM_OK:
+            self._check(rc)
 
     def sttm_paged_attention(self, q, cache: PagedCache, sequences: Sequences, out, scale: float, key_bias=None, weights_in=None,
                              weights_out=None, lse=None, workspace=None):
         """q, out [batch, q_heads, d]; key_bias, weights_in, weights_out float32 [batch, kv_heads, slots]; lse float32
         [batch, q_heads]; workspace: sttm_paged_attention_workspace_bytes() bytes."""
-        self._on_device(q)
-        batch, dev = sequences.batch, q.device
-        qs, os_ = _row_stride(q, "q", batch, cache), _row_stride(out, "out", batch, cache)
+        batch, dev, d = sequences.batch, cache.device, cache.head_dim
+        self._on_device(dev)
+        if sequences.device != dev or q.dim() != 3:
+            raise SttmError(STTM_ERR_ARG, "sequences on the cache's device, q [batch, q_heads, head_dim]")
         q_heads = q.shape[1]
-        if q.shape[2] != cache.head_dim or out.shape != q.shape:
-            raise SttmError(STTM_ERR_SHAPE, "q must have the cache's head_dim, out q's shape")
-        if sequences.device != dev or (workspace is not None and workspace.device != dev):
-            raise SttmError(STTM_ERR_ARG, "the tensors must be on one device")
-        slots, first = 0, key_bias if key_bias is not None else weights_out
+        qs, os_ = _rows(q, "q", batch, q_heads, d, cache.dtype, dev), _rows(out, "out", batch, q_heads, d, cache.dtype, dev)
+        slots, bias_at, in_at, out_at = 0, None, None, None
+        first = key_bias if key_bias is not None else weights_out if weights_out is not None else weights_in
         if first is not None:
             slots = first.shape[-1]
             shape = (batch, cache.kv_heads, slots)
-            _slot_table(key_bias, "key_bias", torch.float32, shape, dev)
-            _slot_table(weights_in, "weights_in", torch.float32, shape, dev)
-            _slot_table(weights_out, "weights_out", torch.float32, shape, dev)
-        _vector(lse, "lse", torch.float32, batch * q_heads, dev)
-        self._check(_lib.sttm_paged_attention(self._h, cache.struct, sequences.struct, q_heads, scale, _ptr(q), qs, _ptr(key_bias),
-                                              _ptr(weights_in), _ptr(weights_out), slots, _ptr(out), os_, _ptr(lse), _ptr(workspace),
-                                              workspace.nbytes if workspace is not None else 0))
+            bias_at = _table(key_bias, "key_bias", torch.float32, shape, dev)
+            in_at = _table(weights_in, "weights_in", torch.float32, shape, dev)
+            out_at = _table(weights_out, "weights_out", torch.float32, shape, dev)
+        ws, size = self._scratch(workspace, dev)
+        rc = _lib.sttm_paged_attention(self._h, cache.ref, sequences.ref, q_heads, scale, q.data_ptr(), qs, bias_at, in_at, out_at,
+                                       slots, out.data_ptr(), os_, _vector(lse, "lse", torch.float32, batch * q_heads, dev), ws, size)
+        if rc != STTM_OK:
+            self._check(rc)
 
     def sttm_cache_evict(self, cache: PagedCache, sequences: Sequences, keep, lengths_out, weights_in, weights_out, ids_in, ids_out,
                          total=None, sink: int = 0, recent: int = 0, bias_in=None, bias_out=None, workspace=None):
         """keep, total, lengths_out int32 [batch]; weights_*, bias_* float32 and ids_* int32 [batch, kv_heads, slots];
         workspace: sttm_cache_evict_workspace_bytes() bytes."""
-        self._on_device(cache)
-        batch, dev = sequences.batch, cache.device
-        if sequences.device != dev or (workspace is not None and workspace.device != dev):
-            raise SttmError(STTM_ERR_ARG, "the tensors must be on one device")
-        _vector(keep, "keep", torch.int32, batch, dev)
-        _vector(total, "total", torch.int32, batch, dev)
-        _vector(lengths_out, "lengths_out", torch.int32, batch, dev)
+        batch, dev, f32, i32 = sequences.batch, cache.device, torch.float32, torch.int32
+        self._on_device(dev)
+        if sequences.device != dev:
+            raise SttmError(STTM_ERR_ARG, "sequences on the cache's device")
         shape = (batch, cache.kv_heads, weights_in.shape[-1])
-        _slot_table(weights_in, "weights_in", torch.float32, shape, dev)
-        _slot_table(weights_out, "weights_out", torch.float32, shape, dev)
-        _slot_table(ids_in, "ids_in", torch.int32, shape, dev)
-        _slot_table(ids_out, "ids_out", torch.int32, shape, dev)
-        _slot_table(bias_in, "bias_in", torch.float32, shape, dev)
-        _slot_table(bias_out, "bias_out", torch.float32, shape, dev)
-        self._check(_lib.sttm_cache_evict(self._h, cache.struct, sequences.struct, _ptr(keep), _ptr(total), sink, recent, shape[2],
-                                          _ptr(weights_in), _ptr(weights_out), _ptr(ids_in), _ptr(ids_out), _ptr(bias_in),
-                                          _ptr(bias_out), _ptr(lengths_out), _ptr(workspace),
-                                          workspace.nbytes if workspace is not None else 0))
+        ws, size = self._scratch(workspace, dev)
+        rc = _lib.sttm_cache_evict(self._h, cache.ref, sequences.ref, _vector(keep, "keep", i32, batch, dev),
+                                   _vector(total, "total", i32, batch, dev), sink, recent, shape[2],
+                                   _table(weights_in, "weights_in", f32, shape, dev), _table(weights_out, "weights_out", f32, shape, dev),
+                                   _table(ids_in, "ids_in", i32, shape, dev), _table(ids_out, "ids_out", i32, shape, dev),
+                                   _table(bias_in, "bias_in", f32, shape, dev), _table(bias_out, "bias_out", f32, shape, dev),
+                                   _vector(lengths_out, "lengths_out", i32, batch, dev), ws, size)
+        if rc != STTM_OK:
+            self._check(rc)
 
     def sttm_export(self, table, dst):
         self._check(_lib.sttm_export(self._h, table, _ptr(dst), dst.numel() * dst.element_size()))

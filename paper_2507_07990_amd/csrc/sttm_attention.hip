@@ -10,7 +10,7 @@ namespace {
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kQTile = 16;      // heads of a group that one matrix product takes
 constexpr int kChunkStep = 128; // a chunk is a multiple of this many slots: a block of 32 for each wavefront
-constexpr int kChunkMax = 1024;
+constexpr int kChunkMax = 512;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 typedef float f32x4 __attribute__((vector_size(16)));
@@ -203,10 +203,18 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   // end on are read as the last one. Loads stand without a branch around them: they are on their way together.
   u32x4 k[TILES][NQ];
   ValueRow<DT, VW> v[TILES][4];
-  bool outside = false, dead[TILES][4];
-  float add[TILES][4];
+  bool outside = false, dead_next[TILES][4];
+  float add_next[TILES][4];
   auto load_keys = [&](int s0) {
     outside = false;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int slot = s0 + 16 * t + 4 * g + r;
+        add_next[t][r] = BIAS ? bias[min(slot, end - 1)] : 0.f;
+        dead_next[t][r] = slot >= end;
+      }
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       const int slot = min(s0 + 16 * t + i16, end - 1);
@@ -223,6 +231,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
       }
     }
   };
+  bool gone[TILES][4];
   auto load_values = [&](int s0) {
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
@@ -230,8 +239,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
       for (int r = 0; r < 4; ++r) {
         const int slot = s0 + 16 * t + 4 * g + r, in = min(slot, end - 1);
         const long long at = page_at[(in - first) >> a.pool.shift];
-        add[t][r] = BIAS ? bias[in] : 0.f;
-        dead[t][r] = slot >= end || at < 0;
+        gone[t][r] = at < 0;
         v[t][r].load(a.pool.v + (at < 0 ? 0 : at) + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
       }
   };
@@ -242,28 +250,39 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   }
   for (int s0 = start; s0 < end; s0 += kAttnWaves * BLOCK) {
     const bool careful = BIAS || s0 + BLOCK > end || __ballot(outside) != 0;  // (the same in all lanes: masked slots among these)
-    if (careful) {
+    bool dead[TILES][4];
+    float add[TILES][4];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        add[t][r] = add_next[t][r];
+        dead[t][r] = dead_next[t][r] || gone[t][r] || (BIAS && add[t][r] == -INFINITY);
+      }
+    auto clear_dead = [&]() {
 #pragma unroll
       for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          dead[t][r] |= add[t][r] == -INFINITY;
+        for (int r = 0; r < 4; ++r)
           if (dead[t][r]) v[t][r].clear();
-        }
-    }
+    };
+    if (!BIAS && careful) clear_dead();  // (no branch between the products and what reads them: this compiler puts no wait
+                                         // states across one, and the result would be read before it is there)
     f32x4 s[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 part[2] = {s[t], s[t]};  // (fp32: two chains of products, each waits for its own)
 #pragma unroll
       for (int c = 0; c < NQ; ++c) {
         if constexpr (DT == 0) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[t] = mma32(__uint_as_float(k[t][c][j]), __uint_as_float(q[c][j]), s[t]);
+          for (int j = 0; j < 4; ++j) part[j % 2] = mma32(__uint_as_float(k[t][c][j]), __uint_as_float(q[c][j]), part[j % 2]);
         } else {
           s[t] = mma16<DT>(k[t][c], q[c], s[t]);
         }
       }
+      if constexpr (DT == 0) s[t] = part[0] + part[1];
     }
     load_keys(s0 + kAttnWaves * BLOCK);  // (the next block's, while this one goes on; past the end the last slot)
     float top = -INFINITY;
@@ -303,6 +322,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
         p[t][r] = exp2_fast((s[t][r] - base) * a.unit);
         l += p[t][r];
       }
+    if constexpr (BIAS) clear_dead();
     if constexpr (DT == 0) {
 #pragma unroll
       for (int n = 0; n < VW; ++n)

@@ -152,29 +152,32 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_mark(EvictArgs a) {
   }
   if (blockIdx.x == 0 && tid == 0) a.found[row] = make_int4(digit, left, count, 0);
   const bool exact = !search || left == count, listed = !exact && count <= kListMost;
-  constexpr int GROUP = 8, RUN = kPartSlots / (kPartThreads / kWave);
+  constexpr int RUN = kPartSlots / (kPartThreads / kWave), STEPS = RUN / kWave;
   const int start = first + wave * RUN, end = min(length, start + RUN);
+  uint32_t key[STEPS];
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) key[k] = search ? a.keys[row * a.seqs.max_len + min(start + k * kWave + lane, length - 1)] : 0u;
+  int near = 0;  // of this wavefront: one place in the list is taken for all of them
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const int s = start + k * kWave, i = s + lane, d = (int)(key[k] >> (32 - kDigitBits));
+    const unsigned long long mask = __ballot(i < end && (search ? d > digit || (exact && d == digit) : stay > 0));
+    if (lane == 0 && s < end) a.stays[row * a.words + (s >> 6)] = mask;
+    near += __popcll(__ballot(i < end && d == digit));
+  }
+  if (!listed || near == 0) return;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(a.listed + row, near);
+  at = lane_value(at, 0);
   const unsigned long long below = (1ull << lane) - 1;
-  uint2* list = a.list + row * kListMost;
-  for (int s0 = start; s0 < end; s0 += GROUP * kWave) {
-    uint32_t key[GROUP];
 #pragma unroll
-    for (int k = 0; k < GROUP; ++k) key[k] = search ? a.keys[row * a.seqs.max_len + min(s0 + k * kWave + lane, length - 1)] : 0u;
-#pragma unroll
-    for (int k = 0; k < GROUP; ++k) {
-      const int s = s0 + k * kWave, i = s + lane, d = (int)(key[k] >> (32 - kDigitBits));
-      if (s >= end) break;
-      const bool yes = i < end && (search ? d > digit || (exact && d == digit) : stay > 0);
-      const unsigned long long mask = __ballot(yes);
-      if (lane == 0) a.stays[row * a.words + (s >> 6)] = mask;
-      const unsigned long long near = __ballot(listed && i < end && d == digit);
-      if (near) {
-        int at = 0;
-        if (lane == 0) at = atomicAdd(a.listed + row, (int)__popcll(near));
-        at = lane_value(at, 0) + __popcll(near & below);
-        if ((near >> lane & 1) && at < kListMost) list[at] = make_uint2(key[k], (unsigned)i);
-      }
-    }
+  for (int k = 0; k < STEPS; ++k) {
+    const int i = start + k * kWave + lane;
+    const bool mine = i < end && (int)(key[k] >> (32 - kDigitBits)) == digit;
+    const unsigned long long mask = __ballot(mine);
+    const int place = at + __popcll(mask & below);
+    if (mine && place < kListMost) a.list[row * kListMost + place] = make_uint2(key[k], (unsigned)i);
+    at += __popcll(mask);
   }
 }
 

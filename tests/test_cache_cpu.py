@@ -20,7 +20,7 @@ def bench():
     binding._lib = binding._declare(ctypes.CDLL(build_cache_cpu.build()))
     try:
         ctx = binding.Sttm(0, stream_ptr=0)
-        ctx.device = None                       # (host tensors)
+        ctx._device_index = -1                  # (host tensors)
         yield C.Bench(binding, ctx, "cpu")
         ctx.close()
     finally:
