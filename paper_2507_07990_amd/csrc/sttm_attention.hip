@@ -9,8 +9,7 @@ namespace {
 
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kQTile = 16;      // heads of a group that one matrix product takes
-constexpr int kChunkStep = 128; // a chunk is a multiple of this many slots: a block of 32 for each wavefront
-constexpr int kChunkMax = 512;
+constexpr int kChunkMax = 512;  // slots of one workgroup at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 typedef float f32x4 __attribute__((vector_size(16)));
@@ -162,6 +161,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   __shared__ long long page_at[kChunkMax / 8];        // byte offset of every page of the chunk, -1: not in the pool
   __shared__ float joined[kAttnWaves][PART * 4][kWave];  // the wavefronts' sums, a part of the channels at a time
   __shared__ float stat_m[kAttnWaves][kQTile], stat_l[kAttnWaves][kQTile];
+  __shared__ float2 all_heads[kQTile];  // maximum and reciprocal sum
 
   const int b = blockIdx.z, h = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles, chunk = blockIdx.x;
   const int length = seq_length(a.seqs, b);
@@ -372,6 +372,16 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     if (!a.part && a.lse) a.lse[head] = top == -INFINITY ? -INFINITY : top * a.natural + logf(total);
   }
   const float share = a.part ? 1.f : total == 0.f ? 0.f : 1.f / total;
+  if (logits && !a.stat) {  // one chunk and one tile: every slot's weight from here
+    if (tid < heads) all_heads[tid] = make_float2(top == -INFINITY ? 0.f : top, share);
+    __syncthreads();
+    const long long slots = ((long long)b * a.kv_heads + h) * a.slot_stride;
+    for (int slot = tid; slot < end; slot += kAttnThreads) {
+      float sum = 0.f;
+      for (int i = 0; i < heads; ++i) sum = fmaf(exp2_fast((logits[(long long)slot * a.group + i] - all_heads[i].x) * a.unit), all_heads[i].y, sum);
+      a.weights_out[slots + slot] = (a.weights_in ? a.weights_in[slots + slot] : 0.f) + sum;
+    }
+  }
 #pragma unroll
   for (int n0 = 0; n0 < VW; n0 += PART) {
     if (n0) __syncthreads();
@@ -394,6 +404,185 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
       }
       if (a.part) *reinterpret_cast<float4*>(a.part + (head * a.chunks + chunk) * a.d + channel) = make_float4(x[0], x[1], x[2], x[3]);
       else store_channels<DT>(a.out + b * a.out_stride + (((long long)h * a.group + head0 + i16) * a.d + channel) * ES, x);
+    }
+  }
+}
+
+// The sum over the sixteen lanes of a row, the same bits in each of them.
+__device__ inline float row16_sum(float v) {
+#ifndef STTM_HOST_EMULATION
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xF, 0xF, true));  // row_ror:8
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x124, 0xF, 0xF, true));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x122, 0xF, 0xF, true));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x121, 0xF, 0xF, true));
+#else
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+#endif
+  return v;
+}
+
+// fp32 with one or two heads a kv head: of the sixteen columns of a matrix product one or two would be of use, and in fp32
+// that is what bounds it (56 products of 32 cycles for 16 slots of 72 channels). Here sixteen lanes have a slot's row, keys and
+// values alike, a wavefront four rows at a time, and each sixteen lanes their own running maximum and sum over their slots.
+template <int HEADS, int VW, bool BIAS>
+__global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnArgs a) {
+  constexpr int ROWS = 4, BLOCK = 4 * ROWS;  // rows of sixteen lanes under way together
+  __shared__ long long page_at[kChunkMax / 8];
+  __shared__ float joined[kAttnWaves][HEADS][VW][16];
+  __shared__ float stat_m[4 * kAttnWaves][HEADS], stat_l[4 * kAttnWaves][HEADS];
+  __shared__ float2 all_heads[HEADS];
+  const int b = blockIdx.z, h = blockIdx.y, chunk = blockIdx.x;
+  const int length = seq_length(a.seqs, b), first = chunk * a.chunk;
+  if (first >= length && chunk > 0) return;
+  const int end = min(length, first + a.chunk);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g = lane >> 4;
+  for (int p = tid; p << a.pool.shift < end - first; p += kAttnThreads) {
+    const int page = a.seqs.table[b * a.seqs.table_stride + (first >> a.pool.shift) + p];
+    const bool ok = page >= 0 && page < a.pool.pages;
+    page_at[p] = ok ? page * a.pool.page_stride + h * a.pool.head_stride : -1;
+  }
+  // Channel 64 * (n / 4) + 4 * i16 + n % 4 of each head; zero beyond the row, and for a head that is not there.
+  float q[HEADS][VW], acc[HEADS][VW], m[HEADS], l[HEADS];
+#pragma unroll
+  for (int e = 0; e < HEADS; ++e) {
+    const char* row = a.q + b * a.q_stride + ((long long)h * a.group + min(e, a.group - 1)) * a.d * 4;
+    ValueRow<0, VW> x;
+    x.load(row, i16, a.pool.row);
+#pragma unroll
+    for (int n = 0; n < VW; ++n) {
+      q[e][n] = 64 * (n / 4) + 4 * i16 < a.d ? __uint_as_float(x.w[n]) : 0.f;
+      acc[e][n] = 0.f;
+    }
+    m[e] = -INFINITY;
+    l[e] = 0.f;
+  }
+  __syncthreads();
+  const int page_mask = (1 << a.pool.shift) - 1;
+  const float* bias = BIAS ? a.bias + ((long long)b * a.kv_heads + h) * a.slot_stride : nullptr;
+  float* logits = a.logits ? a.logits + ((long long)b * a.kv_heads + h) * a.seqs.max_len * a.group : nullptr;
+  ValueRow<0, VW> k[ROWS], v[ROWS];
+  float add[ROWS];
+  bool dead[ROWS];
+  auto load = [&](int s0) {  // (slots from the end on are read as the last one)
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int slot = s0 + ROWS * g + r, in = min(slot, end - 1);
+      const long long at = page_at[(in - first) >> a.pool.shift];
+      const long long off = (at < 0 ? 0 : at) + (in & page_mask) * a.pool.token_stride;
+      add[r] = BIAS ? bias[in] : 0.f;
+      dead[r] = slot >= end || at < 0;
+      k[r].load(a.pool.k + off, i16, a.pool.row);
+      v[r].load(a.pool.v + off, i16, a.pool.row);
+    }
+  };
+  const int start = first + wave * BLOCK;
+  if (start < end) load(start);
+  for (int s0 = start; s0 < end; s0 += kAttnWaves * BLOCK) {
+    float s[HEADS][ROWS], p[HEADS][ROWS];
+    bool gone[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      gone[r] = dead[r] || (BIAS && add[r] == -INFINITY);
+#pragma unroll
+      for (int e = 0; e < HEADS; ++e) {
+        float x = 0.f;
+#pragma unroll
+        for (int n = 0; n < VW; ++n)
+          x = fmaf(64 * (n / 4) + 4 * i16 < a.d ? __uint_as_float(k[r].w[n]) : 0.f, q[e][n], x);
+        x = row16_sum(x);
+        x = BIAS ? fmaf(x, a.scale, add[r]) : x * a.scale;
+        s[e][r] = gone[r] ? -INFINITY : x;
+      }
+    }
+    if (logits) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int e = 0; e < HEADS; ++e)
+          if (i16 == e && e < a.group && s0 + ROWS * g + r < end) logits[(long long)(s0 + ROWS * g + r) * a.group + e] = s[e][r];
+    }
+#pragma unroll
+    for (int e = 0; e < HEADS; ++e) {
+      float top = m[e];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) top = fmaxf(top, s[e][r]);
+      if (__ballot(top > m[e]) != 0) {  // (seldom after the first blocks)
+        const float shrink = factor(m[e], top, a.unit);
+        m[e] = top;
+        l[e] *= shrink;
+#pragma unroll
+        for (int n = 0; n < VW; ++n) acc[e][n] *= shrink;
+      }
+      const float base = m[e] == -INFINITY ? 0.f : m[e];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        p[e][r] = exp2_fast((s[e][r] - base) * a.unit);
+        l[e] += p[e][r];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int n = 0; n < VW; ++n) {
+        const float x = gone[r] ? 0.f : __uint_as_float(v[r].w[n]);
+#pragma unroll
+        for (int e = 0; e < HEADS; ++e) acc[e][n] = fmaf(p[e][r], x, acc[e][n]);
+      }
+    load(s0 + kAttnWaves * BLOCK);
+  }
+
+  // Sixteen sums a head (four wavefronts of four rows) on a common maximum: the rows by lanes, the wavefronts in their order.
+  if (i16 == 0) {
+#pragma unroll
+    for (int e = 0; e < HEADS; ++e) {
+      stat_m[4 * wave + g][e] = m[e];
+      stat_l[4 * wave + g][e] = l[e];
+    }
+  }
+  __syncthreads();
+  float share[HEADS];
+#pragma unroll
+  for (int e = 0; e < HEADS; ++e) {
+    float top = -INFINITY, total = 0.f;
+    for (int w = 0; w < 4 * kAttnWaves; ++w) top = fmaxf(top, stat_m[w][e]);
+    for (int w = 0; w < 4 * kAttnWaves; ++w) total += stat_l[w][e] * factor(stat_m[w][e], top, a.unit);
+    const float mine = factor(m[e], top, a.unit);
+#pragma unroll
+    for (int n = 0; n < VW; ++n) {
+      float x = acc[e][n] * mine;
+      x += __shfl_xor(x, 16, 64);
+      x += __shfl_xor(x, 32, 64);
+      if (g == 0) joined[wave][e][n][i16] = x;
+    }
+    share[e] = a.part ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    if (tid == 0 && e < a.group) {
+      const long long head = ((long long)b * a.kv_heads + h) * a.group + e;
+      if (a.stat) a.stat[head * a.chunks + chunk] = make_float2(top, total);
+      if (!a.part && a.lse) a.lse[head] = top == -INFINITY ? -INFINITY : top * a.natural + logf(total);
+      all_heads[e] = make_float2(top == -INFINITY ? 0.f : top, share[e]);
+    }
+  }
+  __syncthreads();
+  if (logits && !a.stat) {
+    const long long slots = ((long long)b * a.kv_heads + h) * a.slot_stride;
+    for (int slot = tid; slot < end; slot += kAttnThreads) {
+      float sum = 0.f;
+      for (int e = 0; e < a.group; ++e) sum = fmaf(exp2_fast((logits[(long long)slot * a.group + e] - all_heads[e].x) * a.unit), all_heads[e].y, sum);
+      a.weights_out[slots + slot] = (a.weights_in ? a.weights_in[slots + slot] : 0.f) + sum;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < HEADS; ++e) {
+    if (e >= a.group) continue;
+    const long long head = ((long long)b * a.kv_heads + h) * a.group + e;
+    for (int c = tid; c < a.d; c += kAttnThreads) {
+      const int n = c / 64 * 4 + c % 4, i = c % 64 / 4;
+      float x = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w) x += joined[w][e][n][i];
+      x *= share[e];
+      if (a.part) a.part[(head * a.chunks + chunk) * a.d + c] = x;
+      else *reinterpret_cast<float*>(a.out + b * a.out_stride + (((long long)h * a.group + e) * a.d + c) * 4) = x;
     }
   }
 }
@@ -498,6 +687,7 @@ __global__ void __launch_bounds__(kFinishThreads) k_attention_finish(AttnArgs a,
 
 struct Plan {
   int tiles, chunk, chunks;
+  bool whole;                 // a workgroup sees all of a kv head: nothing is left to do behind it
   size_t part, stat, logits, bytes;  // offsets in the workspace
 };
 
@@ -505,17 +695,18 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s, int q_heads, bool w
   Plan p;
   const int group = q_heads / c->kv_heads, max_len = make_seqs(c, s).max_len;
   p.tiles = (group + kQTile - 1) / kQTile;
-  // Chunks for some 1024 workgroups, if there are as many slots.
-  const long long rows = (long long)std::max(s->batch, 1) * c->kv_heads * p.tiles;
-  const long long want = std::max(1ll, 1024 / rows), len = std::max(max_len, 1);
-  long long chunk = ((len + want - 1) / want + kChunkStep - 1) / kChunkStep * kChunkStep;
-  p.chunk = (int)std::min(chunk, (long long)kChunkMax);
+  // One chunk for short sequences: a second launch costs more than the few blocks that follow each other. Else chunks of 256 or
+  // 512 slots, the longer ones where there are enough of them for every compute unit to have several of unequal sequences;
+  // of 128 only where 256 would leave compute units without any.
+  const long long rows = (long long)std::max(s->batch, 1) * c->kv_heads * p.tiles, len = std::max(max_len, 1);
+  p.chunk = len <= kChunkMax || rows * len >= kChunkMax * 4096ll ? kChunkMax : rows * len >= 256 * 256ll ? 256 : 128;
   p.chunks = (int)((len + p.chunk - 1) / p.chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
   const size_t heads = (size_t)s->batch * q_heads;
   p.part = take(p.chunks > 1 ? heads * p.chunks * c->head_dim * sizeof(float) : 0);
-  p.stat = take(p.chunks > 1 || weights ? heads * p.chunks * sizeof(float2) : 0);
+  p.whole = p.chunks == 1 && p.tiles == 1;
+  p.stat = take(p.chunks > 1 || (weights && !p.whole) ? heads * p.chunks * sizeof(float2) : 0);
   p.logits = take(weights ? heads * (size_t)max_len * sizeof(float) : 0);
   p.bytes = std::max(off, (size_t)256);
   return p;
@@ -531,8 +722,18 @@ int check_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences
   return STTM_OK;
 }
 
+template <int HEADS, int VW>
+void launch_rows(const AttnArgs& a, dim3 grid, hipStream_t s) {
+  if (a.bias) hipLaunchKernelGGL((k_paged_attention_rows<HEADS, VW, true>), grid, dim3(kAttnThreads), 0, s, a);
+  else hipLaunchKernelGGL((k_paged_attention_rows<HEADS, VW, false>), grid, dim3(kAttnThreads), 0, s, a);
+}
+
 template <int DT, int NQ, int VW>
 void launch_blocks(const AttnArgs& a, dim3 grid, hipStream_t s) {
+  if constexpr (DT == 0) {
+    if (a.group == 1) return launch_rows<1, VW>(a, grid, s);
+    if (a.group == 2) return launch_rows<2, VW>(a, grid, s);
+  }
   if (a.bias) hipLaunchKernelGGL((k_paged_attention<DT, NQ, VW, true>), grid, dim3(kAttnThreads), 0, s, a);
   else hipLaunchKernelGGL((k_paged_attention<DT, NQ, VW, false>), grid, dim3(kAttnThreads), 0, s, a);
 }
@@ -548,7 +749,7 @@ void launch_attention(const AttnArgs& a, int batch, hipStream_t s) {
   else if (a.d <= 128) launch_blocks<DT, 4 * W, 8>(a, grid, s);
   else if (a.d <= 192) launch_blocks<DT, 6 * W, 16>(a, grid, s);
   else launch_blocks<DT, 8 * W, 16>(a, grid, s);
-  const int joins = a.part ? a.group : 0, weights = a.weights_out ? (a.seqs.max_len + kFinishThreads - 1) / kFinishThreads : 0;
+  const int joins = a.part ? a.group : 0, weights = a.weights_out && a.stat ? (a.seqs.max_len + kFinishThreads - 1) / kFinishThreads : 0;
   if (joins + weights)
     hipLaunchKernelGGL((k_attention_finish<DT>), dim3(joins + weights, a.kv_heads, batch), dim3(kFinishThreads), 0, s, a, joins);
 }
@@ -599,7 +800,7 @@ extern "C" int sttm_paged_attention(sttm_ctx* ctx, const sttm_cache* cache, cons
   a.slot_stride = slot_stride;
   if (weights_out) a.logits = reinterpret_cast<float*>(ws + p.logits);
   if (p.chunks > 1) a.part = reinterpret_cast<float*>(ws + p.part);
-  if (p.chunks > 1 || weights_out) a.stat = reinterpret_cast<float2*>(ws + p.stat);
+  if (p.chunks > 1 || (weights_out && !p.whole)) a.stat = reinterpret_cast<float2*>(ws + p.stat);
   a.unit = key_bias ? kLog2e : 1.f;
   a.natural = key_bias ? 1.f : kLn2;
   a.scale = key_bias ? scale : scale * kLog2e;

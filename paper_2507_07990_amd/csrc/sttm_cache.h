@@ -59,6 +59,17 @@ __device__ inline float exp2_fast(float x) {
 #endif
 }
 
+// An 8-byte store past the caches (see store_once).
+__device__ inline void store_once8(char* p, const uint2& v) {
+#ifndef STTM_HOST_EMULATION
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 x = {v.x, v.y};
+  __builtin_nontemporal_store(x, reinterpret_cast<u32x2*>(p));
+#else
+  *reinterpret_cast<uint2*>(p) = v;
+#endif
+}
+
 // sin and cos of pi * x, |x| <= 1.
 __device__ inline void sincos_half_turns(float x, float* s, float* c) {
 #ifndef STTM_HOST_EMULATION

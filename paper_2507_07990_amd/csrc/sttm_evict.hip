@@ -23,6 +23,7 @@ struct EvictArgs {
   int* listed;                 // [batch, kv_heads]: how many
   unsigned long long* stays;   // [batch, kv_heads, words]: a bit a slot
   int32_t *holes, *movers;     // [batch, kv_heads, pairs]: the j-th mover goes to the j-th hole
+  int32_t* ranks;              // [batch, kv_heads, words]: holes before a word's
   int4* counts;                // [batch, kv_heads]: pairs, new length, length, tokens so far (seqs.lengths may be lengths_out)
   int words, pairs, parts;
 };
@@ -195,6 +196,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   __shared__ unsigned long long list[kListMost], word_s[kEvictThreads];
   __shared__ unsigned list_slot[READY ? kListMost : 1];
   __shared__ int2 base_s[kEvictThreads];
+  __shared__ unsigned long long few[kWave], least_s;
   __shared__ unsigned wave_a[kEvictWaves], wave_b[kEvictWaves], bits[4];  // bits: and, or of the keys that are left
   __shared__ int digit_s, rest_s, count_s, listed_s;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -236,7 +238,10 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   bool in_list = false, marked = false;  // marked: the bits of all slots but those in the list are there
   int listed = 0;
   if (search) {
-    if (tid == 0) listed_s = 0;
+    if (tid == 0) {
+      listed_s = 0;
+      least_s = 0;
+    }
     if constexpr (READY) {
       const int4 found = a.found[row];
       prefix = (unsigned long long)found.x << shift;
@@ -281,6 +286,23 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       if (tid < 4) bits[tid] = tid < 2 ? 0xffffffffu : 0u;
       __syncthreads();
       if (left == count || shift == 0) break;
+      if (in_list && count <= kWave) {
+        // few are left: a wavefront has one a lane, and finds the one that as many as stay are no smaller than
+        if (tid == 0) listed_s = 0;
+        __syncthreads();
+        for (int i = tid; i < listed; i += kEvictThreads)
+          if ((list[i] >> shift) == (prefix >> shift)) few[atomicAdd(&listed_s, 1) & (kWave - 1)] = list[i];
+        __syncthreads();
+        if (wave == 0) {
+          const unsigned long long mine = lane < count ? few[lane] : 0;
+          int above = 0;
+          for (int i = 0; i < count; ++i) above += few[i] >= mine;
+          if (lane < count && above == left) least_s = mine;
+        }
+        __syncthreads();
+        prefix = least_s;
+        break;
+      }
       // those that are left: into the list once they fit it; the bits in which they differ
       unsigned long long all = ~0ull, some = 0;
       const bool gather = !READY && !in_list && count <= kListMost;
@@ -396,12 +418,14 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
     for (int w = 0; w < kEvictWaves; ++w) {
       if (w == wave) {
         base_s[tid] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
+        if (word < words) a.ranks[row * a.words + word] = base_s[tid].x;
       }
       round_holes += (int)wave_a[w];
       round_movers += (int)wave_b[w];
     }
     __syncthreads();
     const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll 4
     for (int w = wave; w < min(kEvictThreads, words - w0); w += kEvictWaves) {
       const int slot0 = (w0 + w) * 64;
       const unsigned long long mask = word_s[w], front = up_to(stay - slot0);
@@ -418,8 +442,10 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   if (tid == 0) a.counts[row] = make_int4(min(min(holes, movers), a.pairs), stay, length, total);
 }
 
-// The tables of the slots that neither move nor are filled, and the pairs: LANES lanes a row of the pool, 16 bytes a lane. A
-// mover's entries are read, written to its hole and cleared by one lane, nobody else touches either: outputs may be inputs.
+// A share of the tables, a slot a thread, then a share of the pairs' rows of the pool, LANES lanes a row, 16 bytes a lane. (Tables
+// and rows in workgroups of their own took 97 us where this takes 73, on the ragged batch of 24 sequences; rows through the
+// caches 102.) A mover's entries are read, written to its hole and cleared by one lane, nobody else touches either: outputs
+// may be inputs.
 constexpr int kMoveThreads = 256, kMoveRows = 4;  // (rows of a group of lanes under way together)
 template <int LANES>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
@@ -429,16 +455,30 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
   const int stay = count.y, length = count.z, total = count.w;
   if (blockIdx.x == 0 && h == 0 && tid == 0) a.lengths_out[b] = stay;
   for (int i = blockIdx.x * kMoveThreads + tid; i < length; i += gridDim.x * kMoveThreads) {
-    const bool stays = a.stays[row * a.words + (i >> 6)] >> (i & 63) & 1;
-    if (i >= stay) {
-      if (stays) continue;
-      a.weights_out[at + i] = 0.f;
-      a.ids_out[at + i] = -1;
-      if (a.bias_out) a.bias_out[at + i] = 0.f;
-    } else if (stays) {
-      a.weights_out[at + i] = a.weights_in[at + i];
-      a.ids_out[at + i] = slot_number(a, at, i, length, total);
-      if (a.bias_out) a.bias_out[at + i] = a.bias_in[at + i];
+    const int bit = i & 63;
+    const unsigned long long mask = a.stays[row * a.words + (i >> 6)];
+    const bool stays = mask >> bit & 1;
+    if (i >= stay && stays) continue;  // (a mover: cleared by the slot that takes its entries)
+    int from = i >= stay ? -1 : i;     // the slot whose entries this one gets
+    if (i < stay && !stays) {
+      // (all slots of the word before this one are before the new length too)
+      const int j = a.ranks[row * a.words + (i >> 6)] + __popcll(~mask & ((1ull << bit) - 1));
+      from = j < count.x ? a.movers[row * a.pairs + j] : -1;
+    }
+    float w = 0.f, bias = 0.f;
+    int id = -1;
+    if (from >= 0) {
+      w = a.weights_in[at + from];
+      id = slot_number(a, at, from, length, total);
+      if (a.bias_out) bias = a.bias_in[at + from];
+    }
+    a.weights_out[at + i] = w;
+    a.ids_out[at + i] = id;
+    if (a.bias_out) a.bias_out[at + i] = bias;
+    if (from > i) {
+      a.weights_out[at + from] = 0.f;
+      a.ids_out[at + from] = -1;
+      if (a.bias_out) a.bias_out[at + from] = 0.f;
     }
   }
   constexpr int GROUPS = kMoveThreads / LANES;
@@ -467,21 +507,6 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
     }
 #pragma unroll
     for (int r = 0; r < kMoveRows; ++r) {
-      if (unit != 0 || j0 + r * GROUPS >= count.x) continue;
-      const float w = a.weights_in[at + mover[r]];
-      const int id = slot_number(a, at, mover[r], length, total);
-      a.weights_out[at + hole[r]] = w;
-      a.ids_out[at + hole[r]] = id;
-      a.weights_out[at + mover[r]] = 0.f;
-      a.ids_out[at + mover[r]] = -1;
-      if (a.bias_out) {
-        const float bias = a.bias_in[at + mover[r]];
-        a.bias_out[at + hole[r]] = bias;
-        a.bias_out[at + mover[r]] = 0.f;
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < kMoveRows; ++r) {
       if (q[r] < 0) continue;
       const long long to = q[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(hole[r] & mask) * a.pool.token_stride + unit * 16;
       store_once(reinterpret_cast<uint4*>(a.pool.k + to), k[r]);
@@ -492,7 +517,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
 
 struct Plan {
   int words, pairs, parts;
-  size_t keys, digits, found, list, listed, stays, holes, movers, counts, bytes;
+  size_t keys, digits, found, list, listed, ranks, stays, holes, movers, counts, bytes;
 };
 Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   Plan p;
@@ -508,6 +533,7 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   p.list = take(p.parts ? rows * kListMost * sizeof(uint2) : 0);
   p.listed = take(p.parts ? rows * sizeof(int) : 0);
   p.stays = take(rows * p.words * sizeof(unsigned long long));
+  p.ranks = take(rows * p.words * sizeof(int32_t));
   p.holes = take(rows * p.pairs * sizeof(int32_t));
   p.movers = take(rows * p.pairs * sizeof(int32_t));
   p.counts = take(rows * sizeof(int4));
@@ -565,6 +591,7 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   a.recent = recent;
   a.keys = reinterpret_cast<uint32_t*>(ws + p.keys);
   a.stays = reinterpret_cast<unsigned long long*>(ws + p.stays);
+  a.ranks = reinterpret_cast<int32_t*>(ws + p.ranks);
   a.holes = reinterpret_cast<int32_t*>(ws + p.holes);
   a.movers = reinterpret_cast<int32_t*>(ws + p.movers);
   a.counts = reinterpret_cast<int4*>(ws + p.counts);

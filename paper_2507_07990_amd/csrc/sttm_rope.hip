@@ -93,9 +93,14 @@ template <> struct Run<0> {
   __device__ static inline Run of(const float (&x)[8]) {
     return {make_float4(x[0], x[1], x[2], x[3]), make_float4(x[4], x[5], x[6], x[7])};
   }
-  __device__ inline void store(char* p, int o0, int o1) const {
-    *reinterpret_cast<float4*>(p + o0) = a;
-    *reinterpret_cast<float4*>(p + o1) = b;
+  template <bool ONCE> __device__ inline void store(char* p, int o0, int o1) const {
+    if constexpr (ONCE) {
+      store_once(reinterpret_cast<float4*>(p + o0), a);
+      store_once(reinterpret_cast<float4*>(p + o1), b);
+    } else {
+      *reinterpret_cast<float4*>(p + o0) = a;
+      *reinterpret_cast<float4*>(p + o1) = b;
+    }
   }
 };
 template <int DT> struct Run {
@@ -111,26 +116,33 @@ template <int DT> struct Run {
   __device__ static inline Run of(const float (&x)[8]) {
     return {make_uint2(pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])), make_uint2(pack2<DT>(x[4], x[5]), pack2<DT>(x[6], x[7]))};
   }
-  __device__ inline void store(char* p, int o0, int o1) const {
-    *reinterpret_cast<uint2*>(p + o0) = a;
-    *reinterpret_cast<uint2*>(p + o1) = b;
+  template <bool ONCE> __device__ inline void store(char* p, int o0, int o1) const {
+    if constexpr (ONCE) {
+      store_once8(p + o0, a);
+      store_once8(p + o1, b);
+    } else {
+      *reinterpret_cast<uint2*>(p + o0) = a;
+      *reinterpret_cast<uint2*>(p + o1) = b;
+    }
   }
 };
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 256, kRopeWaves = 2048;
+constexpr int64_t kOnceBytes = 32 << 20;  // the eight L2 of the card together
 
 // LANES lanes share a head's row, eight channels a lane: the two runs of four that its four pairs consist of (or eight
 // channels in a row where pairs are neighbours, and behind the rotated part). A wavefront has 64 / LANES rows of the same
 // token side by side, so that cos and sin of a lane's pairs serve all heads it comes by.
 // The angle is position * frequency in turns, in 64 bits, where whole turns are taken off exactly: in 32 bits position 43,264
 // would leave an angle 2^-9 off.
-template <int DT, int LANES>
+template <int DT, int LANES, bool ONCE>
 __global__ void __launch_bounds__(kRopeThreads) k_qk_norm_rope(RopeArgs a) {
   constexpr int ES = DT == 0 ? 4 : 2, ROWS = kWave / LANES;
-  const long long wave = (long long)blockIdx.x * (kRopeThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long row = wave / a.parts;
+  const unsigned wave = blockIdx.x * (kRopeThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned in_n = wave / (unsigned)a.parts;
+  const long long row = in_n;
   if (row >= a.n) return;  // (the same in all lanes)
-  const int part = (int)(wave % a.parts), lane = threadIdx.x & 63, unit = lane & (LANES - 1), sub = lane / LANES;
+  const int part = (int)(wave - in_n * (unsigned)a.parts), lane = threadIdx.x & 63, unit = lane & (LANES - 1), sub = lane / LANES;
   const bool there = unit < a.d / 8, turns = unit < a.pairs / 4;
   const int o0 = ES * (turns && !a.interleaved ? 4 * unit : 8 * unit);
   const int o1 = ES * (turns && !a.interleaved ? a.pairs + 4 * unit : 8 * unit + 4);
@@ -207,19 +219,19 @@ __global__ void __launch_bounds__(kRopeThreads) k_qk_norm_rope(RopeArgs a) {
         x = Run<DT>::of(f);
       }
     }
-    if (kind == 0) x.store(a.q_out + row * a.q_out_stride + (long long)hh * bytes, o0, o1);
-    if (kind == 1 && a.k_out) x.store(a.k_out + row * a.k_out_stride + (long long)hh * bytes, o0, o1);
-    if (kind != 0 && at >= 0) x.store((kind == 1 ? a.pool.k : a.pool.v) + at + hh * a.pool.head_stride, o0, o1);
+    if (kind == 0) x.template store<ONCE>(a.q_out + row * a.q_out_stride + (long long)hh * bytes, o0, o1);
+    if (kind == 1 && a.k_out) x.template store<ONCE>(a.k_out + row * a.k_out_stride + (long long)hh * bytes, o0, o1);
+    if (kind != 0 && at >= 0) x.template store<ONCE>((kind == 1 ? a.pool.k : a.pool.v) + at + hh * a.pool.head_stride, o0, o1);
   }
 }
 
-template <int DT>
+template <int DT, bool ONCE>
 void launch_rope(const RopeArgs& a, int lanes, hipStream_t s) {
   const long long waves = a.n * a.parts;
   const dim3 grid((unsigned)((waves + kRopeThreads / kWave - 1) / (kRopeThreads / kWave))), block(kRopeThreads);
-  if (lanes == 8) hipLaunchKernelGGL((k_qk_norm_rope<DT, 8>), grid, block, 0, s, a);
-  else if (lanes == 16) hipLaunchKernelGGL((k_qk_norm_rope<DT, 16>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_qk_norm_rope<DT, 32>), grid, block, 0, s, a);
+  if (lanes == 8) hipLaunchKernelGGL((k_qk_norm_rope<DT, 8, ONCE>), grid, block, 0, s, a);
+  else if (lanes == 16) hipLaunchKernelGGL((k_qk_norm_rope<DT, 16, ONCE>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_qk_norm_rope<DT, 32, ONCE>), grid, block, 0, s, a);
 }
 
 }  // namespace
@@ -292,13 +304,14 @@ extern "C" int sttm_qk_norm_rope(sttm_ctx* ctx, int dtype, int64_t n, int q_head
   const int steps = (q_heads + 2 * kv_heads + kWave / lanes - 1) / (kWave / lanes);  // rows of heads a token has
   // Few tokens: their heads are spread over wavefronts until there are some for every SIMD.
   a.parts = 1;
-  while (a.parts < steps && n * a.parts < 2048) a.parts *= 2;
+  while (a.parts < steps && n * a.parts < kRopeWaves) a.parts *= 2;
   if (a.parts > steps) a.parts = steps;
+  const bool once = n * (int64_t)(q_heads + (k_out ? kv_heads : 0) + (cache ? 2 * kv_heads : 0)) * head_dim * es > kOnceBytes;
   int rc = ctx_device(ctx);
   if (rc != STTM_OK) return rc;
   const hipStream_t s = ctx_stream(ctx);
-  if (dtype == STTM_F32) launch_rope<0>(a, lanes, s);
-  else if (dtype == STTM_BF16) launch_rope<1>(a, lanes, s);
-  else launch_rope<2>(a, lanes, s);
+  if (dtype == STTM_F32) once ? launch_rope<0, true>(a, lanes, s) : launch_rope<0, false>(a, lanes, s);
+  else if (dtype == STTM_BF16) once ? launch_rope<1, true>(a, lanes, s) : launch_rope<1, false>(a, lanes, s);
+  else once ? launch_rope<2, true>(a, lanes, s) : launch_rope<2, false>(a, lanes, s);
   return ctx_after_launch(ctx);
 }

@@ -116,6 +116,12 @@ ATTENTION = [
     ("f32", 4, 2, 136, 8, (67,), "slots", "empty", True),
     ("bf16", 3, 1, 168, 8, (45,), "pages", "empty", False),
     ("f16", 2, 1, 32, 16, (129,), "padded", "huge", True),
+    ("f32", 6, 2, 72, 16, (33, 90), "pages", "counts", True),      # fp32 with groups
+    ("f32", 3, 1, 256, 8, (70,), "slots", "", True),
+    ("f32", 20, 1, 24, 8, (66, 1), "pages", "", True),
+    ("f32", 7, 1, 128, 16, (600, 40), "pages", "counts", False),
+    ("f32", 4, 4, 192, 8, (530, 5), "padded", "counts", True),     # fp32 without, several chunks
+    ("bf16", 12, 4, 128, 32, (513, 512, 511), "pages", "", True),  # on both sides of one chunk
 ]
 
 
