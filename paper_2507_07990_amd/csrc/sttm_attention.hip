@@ -99,7 +99,8 @@ struct AttnArgs {
 // Softmax statistics of one head over several parts of the slots.
 __device__ inline float factor(float m, float top, float unit) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * unit); }
 
-// A slot's elements as one lane takes them: NV loads of 16 bytes (8 bytes: VW == 4 of 16 bits). A lane whose share lies
+// A slot's elements as one lane takes them, in loads of 16 bytes (8 bytes: VW == 4 of 16 bits), marked as used once: sixteen lanes
+// take whole lines (the keys' pieces of 64 bytes come by a line twice and are left to the caches). A lane whose share lies
 // beyond the row takes the row's start in its place: what it makes of that is not written.
 template <int DT, int VW> struct ValueRow {
   static constexpr int WORDS = DT == 0 ? VW : VW / 2;
@@ -112,7 +113,7 @@ template <int DT, int VW> struct ValueRow {
 #pragma unroll
       for (int h = 0; h < WORDS / 4; ++h) {
         const int o = i * 16 + h * 256;
-        const uint4 x = *reinterpret_cast<const uint4*>(row + (o < bytes ? o : 0));
+        const uint4 x = load_once(reinterpret_cast<const uint4*>(row + (o < bytes ? o : 0)));
         w[4 * h] = x.x; w[4 * h + 1] = x.y; w[4 * h + 2] = x.z; w[4 * h + 3] = x.w;
       }
     }

@@ -161,3 +161,16 @@ def test_a_step_in_a_graph_on_another_stream(lib):
         torch.cuda.synchronize()
         for a, y in zip(s.result(), want):
             assert torch.equal(a, y)
+
+
+def test_the_example_runs_the_operators_together():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "answer_from_reduced_video.py")
+    spec = importlib.util.spec_from_file_location("answer_from_reduced_video", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    from paper_2507_07990_amd import workloads as wl
+    r = example.run(wl.small_variant(wl.CONFIGS[1], T=6, D=1792), keep=0.5, steps=5, cache_keep=0.5)
+    assert r["kept"] <= r["video_tokens"] // 2 and r["cached"] == r["kept"] + 5 and r["steps"] == 10 and r["finite"]
+    assert r["cached_after"] == r["cached"] // 2 + 5 and r["similarity"] > 0.5
