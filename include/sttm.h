@@ -246,7 +246,7 @@ int sttm_positions(sttm_ctx* ctx, const int32_t* cluster_ids_dev, const int32_t*
  * sttm_cache describes a pool of pages. The row of head h, slot s of page p starts at element
  * p*page_stride + h*head_stride + s*token_stride of k and of v and has head_dim elements. Requirements: head_dim % 8 == 0,
  * 8 <= head_dim <= 256; page_size a power of two, 8 .. 1024; k, v and all strides multiples of 16 bytes; 1 <= kv_heads <=
- * 1024; 1 <= pages < 2^31. */
+ * 1024; 1 <= pages < 2^31; page_size * token_stride of less than 2 GiB. */
 typedef struct {
   void* k;  /* device */
   void* v;  /* device */
@@ -325,7 +325,7 @@ size_t sttm_paged_attention_workspace_bytes(const sttm_cache* cache, const sttm_
  * Tables: float weights_in/out and bias_in/out (bias both or neither NULL), int32 ids_in/out (ids_in NULL: all below zero),
  * all [batch, kv_heads, slot_stride]; an output may be its input. Outputs: the tokens that stay, with their numbers; from the
  * new length to the old one weight 0, number -1, bias 0; behind that as they were. lengths_out int32 [batch] (may be
- * the lengths of seqs). No number may occur twice in one (sequence, kv head). Pages that several sequences share must
+ * the lengths of seqs). No number may occur twice in one (sequence, kv head) (which of them stay is open then). Pages that several sequences share must
  * not be among those that change. A slot whose page number lies outside the
  * pool takes part in the order; its rows are not moved.
  * workspace as for sttm_paged_attention, of sttm_cache_evict_workspace_bytes(...) bytes. Asynchronous. */

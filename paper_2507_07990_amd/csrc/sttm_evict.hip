@@ -40,6 +40,25 @@ __device__ inline uint32_t weight_key(float w, int id, int total, const EvictArg
   return w != w ? 0u : float_key(w == 0.f ? 0.f : w);
 }
 
+// A value that is the same in all lanes, in scalar registers; whether this lane is in a mask, and how many below it are.
+__device__ inline unsigned long long in_scalars(unsigned long long v) {
+  return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ inline bool lane_in(unsigned long long mask, int lane) {
+#ifndef STTM_HOST_EMULATION
+  return __builtin_amdgcn_inverse_ballot_w64(mask);
+#else
+  return mask >> lane & 1;
+#endif
+}
+__device__ inline int lanes_below(unsigned long long mask, int lane) {
+#ifndef STTM_HOST_EMULATION
+  return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+#else
+  return __popcll(mask & ((1ull << lane) - 1));
+#endif
+}
+
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
 constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;  // a digit's count a thread
 constexpr int kListMost = 4096;                            // keys that fit the list in LDS
@@ -170,13 +189,12 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_mark(EvictArgs a) {
   int at = 0;
   if (lane == 0) at = atomicAdd(a.listed + row, near);
   at = lane_value(at, 0);
-  const unsigned long long below = (1ull << lane) - 1;
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) {
     const int i = start + k * kWave + lane;
     const bool mine = i < end && (int)(key[k] >> (32 - kDigitBits)) == digit;
     const unsigned long long mask = __ballot(mine);
-    const int place = at + __popcll(mask & below);
+    const int place = at + lanes_below(mask, lane);
     if (mine && place < kListMost) a.list[row * kListMost + place] = make_uint2(key[k], (unsigned)i);
     at += __popcll(mask);
   }
@@ -206,7 +224,6 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   const int its = (length + kEvictThreads - 1) / kEvictThreads, first = wave * its * kWave;  // its <= KEYS
   const int steps = min(its, max(0, (length - first + kWave - 1) / kWave));                  // of this wavefront
   const bool search = stay > 0 && stay < length;
-  const unsigned long long below = (1ull << lane) - 1;
   const uint32_t* stored = a.keys + row * a.seqs.max_len;
   uint32_t key[KEYS ? KEYS : 1];
   if constexpr (KEYS != 0) {
@@ -325,7 +342,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
             int base = 0;
             if (lane == 0) base = atomicAdd(&listed_s, (int)__popcll(mask));
             base = lane_value(base, 0);
-            if (near) list[base + __popcll(mask & below)] = x;
+            if (near) list[base + lanes_below(mask, lane)] = x;
           }
         });
       }
@@ -385,6 +402,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   const int words = (length + 63) / 64;
   auto up_to = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
   int holes = 0, movers = 0;
+  int32_t *hole_list = a.holes + row * a.pairs, *mover_list = a.movers + row * a.pairs;
   for (int w0 = 0; w0 < words; w0 += kEvictThreads) {
     __syncthreads();
     const int word = w0 + tid, s0 = word * 64;
@@ -424,16 +442,14 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       round_movers += (int)wave_b[w];
     }
     __syncthreads();
-    const unsigned long long below = (1ull << lane) - 1;
-#pragma unroll 4
     for (int w = wave; w < min(kEvictThreads, words - w0); w += kEvictWaves) {
       const int slot0 = (w0 + w) * 64;
-      const unsigned long long mask = word_s[w], front = up_to(stay - slot0);
+      const unsigned long long mask = in_scalars(word_s[w]), front = up_to(stay - slot0);
       const unsigned long long hole_mask = ~mask & up_to(length - slot0) & front, mover_mask = mask & ~front;
-      const int2 base = base_s[w];
-      const int i = base.x + __popcll(hole_mask & below), j = base.y + __popcll(mover_mask & below);
-      if ((hole_mask >> lane & 1) && i < a.pairs) a.holes[row * a.pairs + i] = slot0 + lane;
-      if ((mover_mask >> lane & 1) && j < a.pairs) a.movers[row * a.pairs + j] = slot0 + lane;
+      const int i = __builtin_amdgcn_readfirstlane(base_s[w].x) + lanes_below(hole_mask, lane);
+      const int j = __builtin_amdgcn_readfirstlane(base_s[w].y) + lanes_below(mover_mask, lane);
+      if (lane_in(hole_mask, lane) && i < a.pairs) hole_list[i] = slot0 + lane;
+      if (lane_in(mover_mask, lane) && j < a.pairs) mover_list[j] = slot0 + lane;
     }
     holes += round_holes;
     movers += round_movers;

@@ -17,6 +17,8 @@ int check_cache(sttm_ctx* c, const sttm_cache* p) {
   if (p->page_stride < 0 || p->head_stride < 0 || p->token_stride < p->head_dim || p->page_stride > most || p->head_stride > most ||
       p->token_stride > (1 << 20) || p->page_stride % align || p->head_stride % align || p->token_stride % align)
     return ctx_fail(c, STTM_ERR_SHAPE, "cache strides: multiples of 16 bytes, not negative, token_stride from head_dim to 2^20");
+  if (p->page_size * p->token_stride * elem_bytes(p->dtype) >= (1ll << 31))
+    return ctx_fail(c, STTM_ERR_SHAPE, "the slots of a page must lie within 2 GiB of each other");
   if (!aligned16(p->k) || !aligned16(p->v)) return ctx_fail(c, STTM_ERR_ARG, "k and v must be 16-byte aligned");
   return STTM_OK;
 }

@@ -122,6 +122,8 @@ ATTENTION = [
     ("f32", 7, 1, 128, 16, (600, 40), "pages", "counts", False),
     ("f32", 4, 4, 192, 8, (530, 5), "padded", "counts", True),     # fp32 without, several chunks
     ("bf16", 12, 4, 128, 32, (513, 512, 511), "pages", "", True),  # on both sides of one chunk
+    ("f16", 4, 2, 32, 1024, (1500, 1), "pages", "", True),         # several chunks to a page
+    ("f32", 1, 1, 16, 256, (700,), "slots", "counts", False),
 ]
 
 
@@ -363,6 +365,10 @@ def test_refusals_of_the_library(bench):
     _refused(bench, lib.STTM_ERR_ARG, ctx.sttm_paged_attention, z(1, 1, 16), lib.PagedCache(odd, odd), seqs, z(1, 1, 16), 1.0)
     wide = z(2, 1, 8, 18)[..., :16]
     _refused(bench, lib.STTM_ERR_SHAPE, ctx.sttm_paged_attention, z(1, 1, 16), lib.PagedCache(wide, wide), seqs, z(1, 1, 16), 1.0)
+
+    far = lib.PagedCache(z(1, 1, 1024, 16), z(1, 1, 1024, 16))
+    far.struct.token_stride = 1 << 20                              # (described only: refused before anything is read)
+    _refused(bench, lib.STTM_ERR_SHAPE, ctx.sttm_paged_attention, z(1, 1, 16), far, seqs, z(1, 1, 16), 1.0)
 
     cache = lib.PagedCache(z(2, 2, 8, 16), z(2, 2, 8, 16))
     ws = bench.workspace(1 << 16)
