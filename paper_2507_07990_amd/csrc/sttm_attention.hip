@@ -99,13 +99,13 @@ struct AttnArgs {
 // Softmax statistics of one head over several parts of the slots.
 __device__ inline float factor(float m, float top, float unit) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * unit); }
 
-// A slot's elements as one lane takes them, in loads of 16 bytes (8 bytes: VW == 4 of 16 bits), marked as used once: sixteen lanes
-// take whole lines (the keys' pieces of 64 bytes come by a line twice and are left to the caches). A lane whose share lies
-// beyond the row takes the row's start in its place: what it makes of that is not written.
+// A slot's elements as one lane takes them, in loads of 16 bytes (8 bytes: VW == 4 of 16 bits). ONCE: marked as used once; only
+// where rows are made of whole lines, which sixteen lanes take at a time. A lane whose share lies beyond the row takes the
+// row's start in its place: what it makes of that is not written.
 template <int DT, int VW> struct ValueRow {
   static constexpr int WORDS = DT == 0 ? VW : VW / 2;
   uint32_t w[WORDS];
-  __device__ inline void load(const char* row, int i, int bytes) {  // i: lane % 16
+  template <bool ONCE = false> __device__ inline void load(const char* row, int i, int bytes) {  // i: lane % 16
     if constexpr (DT != 0 && VW == 4) {
       const uint2 x = *reinterpret_cast<const uint2*>(row + (i * 8 < bytes ? i * 8 : 0));
       w[0] = x.x; w[1] = x.y;
@@ -113,7 +113,8 @@ template <int DT, int VW> struct ValueRow {
 #pragma unroll
       for (int h = 0; h < WORDS / 4; ++h) {
         const int o = i * 16 + h * 256;
-        const uint4 x = load_once(reinterpret_cast<const uint4*>(row + (o < bytes ? o : 0)));
+        const uint4* at = reinterpret_cast<const uint4*>(row + (o < bytes ? o : 0));
+        const uint4 x = ONCE ? load_once(at) : *at;
         w[4 * h] = x.x; w[4 * h + 1] = x.y; w[4 * h + 2] = x.z; w[4 * h + 3] = x.w;
       }
     }
@@ -157,6 +158,9 @@ template <int DT, int NQ, int VW, bool BIAS>
 __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attention(AttnArgs a) {
   constexpr int ES = DT == 0 ? 4 : 2, TILES = DT == 0 ? 1 : 2, BLOCK = 16 * TILES, PART = VW < 8 ? VW : 8;
   constexpr int PIECES = DT == 0 ? NQ / 2 : NQ;  // (of 32 channels; the shortest row this instance is chosen for:)
+  // Values past the caches where a head's row is a number of whole lines (146 us against 155 on the ragged batch of 24
+  // sequences; fp32 rows of 288 bytes took 32 against 23). Not the keys: their pieces of 64 bytes come by a line twice.
+  constexpr bool ONCE = DT != 0 && PIECES != 1 && PIECES != 3 && PIECES != 6;
   constexpr int LEAST = ES * (PIECES <= 4 ? 32 * PIECES - 24 : PIECES == 6 ? 136 : 200);
 
   __shared__ long long page_at[kChunkMax / 8];        // byte offset of every page of the chunk, -1: not in the pool
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
         const int slot = s0 + 16 * t + 4 * g + r, in = min(slot, end - 1);
         const long long at = page_at[(in - first) >> a.pool.shift];
         gone[t][r] = at < 0;
-        v[t][r].load(a.pool.v + (at < 0 ? 0 : at) + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
+        v[t][r].template load<ONCE>(a.pool.v + (at < 0 ? 0 : at) + (in & page_mask) * a.pool.token_stride, i16, a.pool.row);
       }
   };
   const int start = first + wave * BLOCK;
