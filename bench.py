@@ -28,12 +28,13 @@ HBM_PEAK_GBS = 8000.0
 
 
 def source_digest() -> str:
-    """sha256 over the library's kernel sources: a traffic figure is only quoted for the code it was measured on."""
+    """sha256 over the sources of the merge path: a traffic figure is only quoted for the code it was measured on. (The
+    operators on a paged cache, which this script does not run, are other files.)"""
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2507_07990_amd", "csrc")
     for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")):
+        if name in ("sttm_api.hip", "sttm_dev.h", "sttm_reduce.hip", "sttm_spatial.hip", "sttm_temporal.hip"):
             h.update(name.encode())
             h.update(open(os.path.join(csrc, name), "rb").read())
     return h.hexdigest()
