@@ -96,7 +96,8 @@ __device__ inline void count_digit(unsigned* hist, bool mine, uint32_t digit, in
 }
 
 // Long rows: keys and the counts of their first digit, a workgroup for every kPartSlots slots, so that a few long rows are
-// gone through by many compute units.
+// gone through by many compute units (four rows of 43,328 slots: 7 us here and 9 in k_evict_mark, where one workgroup a row took
+// 40 for as much; parts of 2,048 slots 5 and 10, and 8 and 16 against 9 and 11 on 192 ragged rows).
 __global__ void __launch_bounds__(kPartThreads) k_evict_keys(EvictArgs a) {
   __shared__ unsigned hist[kDigits];
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, first = blockIdx.x * kPartSlots;
@@ -200,12 +201,16 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_mark(EvictArgs a) {
   }
 }
 
-// One workgroup a (sequence, kv head); a wavefront has a run of slots, their keys in registers (KEYS a lane; 0: from the
-// workspace, which k_evict_keys has filled). The smallest key that stays is found by digits of ten bits, each counted in LDS, one thread a digit's count: the
-// first digit is the top one (sign, exponent, a bit of the weight); the keys that share it (a few hundred to a few thousand of
-// a long row) go on in a list in LDS, with ~number below the weight; every further digit starts at the highest bit in which
-// those left differ, so that equal weights or small numbers cost no rounds of their own. It ends when the digits so far cut
-// off exactly as many slots as stay. Then holes and movers are listed in the order of their slots, on ballots.
+// One workgroup a (sequence, kv head); a wavefront has a run of slots, their keys in registers (KEYS a lane; 0: a long row,
+// whose keys k_evict_keys and k_evict_mark have worked out, counted and marked). The smallest key that stays is found by digits
+// of ten bits, each counted in LDS, one thread a digit's count: the first digit is the top one (sign, exponent, a bit of the
+// weight); the keys that share it (a few hundred to a few thousand of a long row) go on in a list in LDS, with ~number below
+// the weight; every further digit starts at the highest bit in which those left differ, so that equal weights or small numbers
+// cost no rounds of their own. It ends when the digits so far cut off exactly as many slots as stay, or 64 keys are left, which
+// one wavefront ranks. Then holes and movers are listed in the order of their slots, a word of marks a step.
+//
+// Bound by the chain of counts and barriers of one workgroup: 15 us for 128 rows of 4,097 slots, 22 for four of 43,328 (6 of
+// them the lists: two stores of half a wavefront's slots for every 64).
 template <int KEYS>
 __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   constexpr bool READY = KEYS == 0;  // keys and the first digit's counts

@@ -79,6 +79,21 @@ def test_qk_norm_rope(bench, case, form):
         assert torch.isnan(y.transpose(1, 2)[~used]).all(), "a slot that no row names was written"
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_qk_norm_rope_without_a_cache(bench, dtype):
+    """Queries and keys alone, into buffers of their own; a norm for one of the two."""
+    gen, n, H, K, d = _gen(4), 6, 5, 2, 48
+    q, k = (torch.randn(n, h, d, generator=gen).to(TYPES[dtype]) for h in (H, K))
+    w = (1 + 0.2 * torch.randn(d, generator=gen)).to(TYPES[dtype])
+    pos, freq = torch.randint(0, 900, (n,), generator=gen, dtype=torch.int32), torch.linspace(1.0, 0.01, d // 2)
+    qo, ko = bench.guarded(torch.zeros_like(q)), bench.guarded(torch.zeros_like(k))
+    bench.ctx.sttm_qk_norm_rope(bench.put(q), bench.put(k), None, qo, k_out=ko, k_weight=bench.put(w), eps=1e-5,
+                                rope=bench.lib.Rope(bench.put(pos), bench.put(freq)))
+    bench.done()
+    close(qo, *C.rope_reference(q, None, 1e-5, pos[:, None], freq, (d // 2,), False, U[dtype]), what="q")
+    close(ko, *C.rope_reference(k, w, 1e-5, pos[:, None], freq, (d // 2,), False, U[dtype]), what="k")
+
+
 def test_qk_norm_rope_of_rows_that_are_not_finite(bench):
     """An infinity or NaN in one head stays in that head; a row of zeros stays zero."""
     gen = _gen(3)
@@ -177,6 +192,24 @@ def test_paged_attention(bench, case):
         want0 = C.attention_reference(q, *C.cache_views(kv, order, d), table, lens, page, scale, bias, None, wout, dtype)
         close(fresh[2], *want0[2], what="weights from zero")
         assert torch.equal(fresh[0].cpu(), got[0].cpu())
+
+
+@pytest.mark.parametrize("dtype,H,K,d", [("bf16", 6, 2, 40), ("f32", 2, 2, 24), ("f32", 9, 3, 64)])
+def test_paged_attention_of_rows_with_gaps_and_without_lse(bench, dtype, H, K, d):
+    """Queries and results whose rows lie further apart; what is between them stays."""
+    gen, lib, page, lengths = _gen(d), bench.lib, 16, (37, 600, 0)
+    kv, table = C.pool(gen, dtype, K, d, page, lengths)
+    lens, B, gap = torch.tensor(lengths, dtype=torch.int32), len(lengths), 24
+    q = torch.randn(B, H * d + gap, generator=gen).to(TYPES[dtype])
+    out = bench.guarded(torch.full_like(q, 5.0))
+    rows = lambda t: t[:, :H * d].unflatten(1, (H, d))   # noqa: E731
+    cache, seqs = lib.PagedCache(*[bench.put(x) for x in kv]), lib.Sequences(bench.put(table), bench.put(lens), max(lengths))
+    bench.ctx.sttm_paged_attention(rows(bench.put(q)), cache, seqs, rows(out), 0.2,
+                                   workspace=bench.workspace(lib.sttm_paged_attention_workspace_bytes(cache, seqs, H)))
+    bench.done()
+    want = C.attention_reference(rows(q), *kv, table, lens, page, 0.2, None, None, None, dtype)
+    close(rows(out), *want[0], what="out")
+    assert (out[:, H * d:] == 5.0).all()
 
 
 def test_paged_attention_with_pages_outside_of_the_pool(bench):
