@@ -59,11 +59,10 @@ __device__ inline int lanes_below(unsigned long long mask, int lane) {
 #endif
 }
 
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
-constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;  // a digit's count a thread
+constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
 constexpr int kListMost = 4096;                            // keys that fit the list in LDS
 constexpr int kPartThreads = 256, kPartSlots = 4096;       // of one workgroup that works out keys
-constexpr int kKeysHere = 8;                               // keys a lane of a row that is gone through by one workgroup alone
+constexpr int kSlotsHere = 8192;                           // rows up to here are gone through by one workgroup alone
 
 // GROUP keys of a lane, 64 slots apart from `from` on; all loads under way together.
 template <int GROUP>
@@ -211,22 +210,23 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_mark(EvictArgs a) {
 //
 // Bound by the chain of counts and barriers of one workgroup: 15 us for 128 rows of 4,097 slots, 22 for four of 43,328 (6 of
 // them the lists: two stores of half a wavefront's slots for every 64).
-template <int KEYS>
-__global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
+template <int KEYS, int THREADS>  // (KEYS 0 or 8)
+__global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
   constexpr bool READY = KEYS == 0;  // keys and the first digit's counts
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = 8, WAVES = THREADS / kWave, PER = kDigits / THREADS;  // digits' counts a thread
+  constexpr int LIST = KEYS != 0 && KEYS * THREADS < kListMost ? KEYS * THREADS : kListMost;
   __shared__ unsigned hist[kDigits];
-  __shared__ unsigned long long list[kListMost], word_s[kEvictThreads];
+  __shared__ unsigned long long list[LIST], word_s[THREADS];
   __shared__ unsigned list_slot[READY ? kListMost : 1];
-  __shared__ int2 base_s[kEvictThreads];
+  __shared__ int2 base_s[THREADS];
   __shared__ unsigned long long few[kWave], least_s;
-  __shared__ unsigned wave_a[kEvictWaves], wave_b[kEvictWaves], bits[4];  // bits: and, or of the keys that are left
+  __shared__ unsigned wave_a[WAVES], wave_b[WAVES], bits[4];  // bits: and, or of the keys that are left
   __shared__ int digit_s, rest_s, count_s, listed_s;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
   const int length = seq_length(a.seqs, b), total = a.total ? a.total[b] : length;
   const int stay = min(length, max(a.keep[b], 0));
-  const int its = (length + kEvictThreads - 1) / kEvictThreads, first = wave * its * kWave;  // its <= KEYS
+  const int its = (length + THREADS - 1) / THREADS, first = wave * its * kWave;  // its <= KEYS
   const int steps = min(its, max(0, (length - first + kWave - 1) / kWave));                  // of this wavefront
   const bool search = stay > 0 && stay < length;
   const uint32_t* stored = a.keys + row * a.seqs.max_len;
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       if (left != found.z && marked) {
         listed = found.z;
         in_list = true;
-        for (int i = tid; i < listed; i += kEvictThreads) {
+        for (int i = tid; i < listed; i += THREADS) {
           const uint2 x = a.list[row * kListMost + i];
           list[i] = whole_key(x.x, slot_number(a, at, (int)x.y, length, total));
           list_slot[i] = x.y;
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       }
       if (tid == 0) count_s = found.z;
     } else {
-      hist[tid] = 0;
+      for (int i = tid; i < kDigits; i += THREADS) hist[i] = 0;
       __syncthreads();
       each(false, [&](int, int, bool there, uint32_t k, int) { count_digit(hist, there, k >> (32 - kDigitBits), lane); });
     }
@@ -289,15 +289,25 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       __syncthreads();
       if (!picked) {
         // the digit at which the counts from the top reach `left`
-        const unsigned sum = hist[kDigits - 1 - tid];
+        unsigned n[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          n[i] = hist[kDigits - 1 - tid * PER - i];
+          sum += n[i];
+        }
         unsigned upto = wave_inclusive(sum, lane);
         if (lane == 63) wave_a[wave] = upto;
         __syncthreads();
         for (int w = 0; w < wave; ++w) upto += wave_a[w];
-        if (upto >= (unsigned)left && upto - sum < (unsigned)left) {  // one thread's
-          digit_s = kDigits - 1 - tid;
-          rest_s = left - (int)(upto - sum);
-          count_s = (int)sum;
+        unsigned before = upto - sum;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          if (before < (unsigned)left && before + n[i] >= (unsigned)left) {  // one thread's
+            digit_s = kDigits - 1 - tid * PER - i;
+            rest_s = left - (int)before;
+            count_s = (int)n[i];
+          }
+          before += n[i];
         }
         __syncthreads();
         prefix |= (unsigned long long)digit_s << shift;
@@ -312,7 +322,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
         // few are left: a wavefront has one a lane, and finds the one that as many as stay are no smaller than
         if (tid == 0) listed_s = 0;
         __syncthreads();
-        for (int i = tid; i < listed; i += kEvictThreads)
+        for (int i = tid; i < listed; i += THREADS)
           if ((list[i] >> shift) == (prefix >> shift)) few[atomicAdd(&listed_s, 1) & (kWave - 1)] = list[i];
         __syncthreads();
         if (wave == 0) {
@@ -327,9 +337,9 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       }
       // those that are left: into the list once they fit it; the bits in which they differ
       unsigned long long all = ~0ull, some = 0;
-      const bool gather = !READY && !in_list && count <= kListMost;
+      const bool gather = !READY && !in_list && count <= LIST;
       if (in_list) {
-        for (int i = tid; i < listed; i += kEvictThreads) {
+        for (int i = tid; i < listed; i += THREADS) {
           const unsigned long long k = list[i];
           if ((k >> shift) == (prefix >> shift)) { all &= k; some |= k; }
         }
@@ -361,7 +371,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
         }
       if (lane < 2) atomicAnd(&bits[lane], lane ? v[1] : v[0]);
       else if (lane < 4) atomicOr(&bits[lane], lane == 3 ? v[3] : v[2]);
-      hist[tid] = 0;
+      for (int i = tid; i < kDigits; i += THREADS) hist[i] = 0;
       __syncthreads();
       if (gather) {
         in_list = true;
@@ -380,7 +390,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       const unsigned long long agree = prefix >> shift >> kDigitBits, settled = prefix >> above;
       auto left_over = [&](unsigned long long k) { return (k >> shift >> kDigitBits) == agree && (k >> above) == settled; };
       if (in_list) {
-        for (int i0 = 0; i0 < listed; i0 += kEvictThreads) {
+        for (int i0 = 0; i0 < listed; i0 += THREADS) {
           const int i = i0 + tid;
           const unsigned long long k = i < listed ? list[i] : 0;
           count_digit(hist, i < listed && left_over(k), (uint32_t)(k >> shift) & (kDigits - 1), lane);
@@ -408,16 +418,16 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
   auto up_to = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
   int holes = 0, movers = 0;
   int32_t *hole_list = a.holes + row * a.pairs, *mover_list = a.movers + row * a.pairs;
-  for (int w0 = 0; w0 < words; w0 += kEvictThreads) {
+  for (int w0 = 0; w0 < words; w0 += THREADS) {
     __syncthreads();
     const int word = w0 + tid, s0 = word * 64;
     if (word < words) word_s[tid] = a.stays[row * a.words + word];
     __syncthreads();
     if (in_list && marked) {
       unsigned* half = reinterpret_cast<unsigned*>(word_s);
-      for (int i = tid; i < listed; i += kEvictThreads) {
+      for (int i = tid; i < listed; i += THREADS) {
         const int at_word = (int)(list_slot[i] >> 6) - w0;
-        if (list[i] >= prefix && at_word >= 0 && at_word < kEvictThreads) atomicOr(&half[2 * at_word + (list_slot[i] >> 5 & 1)], 1u << (list_slot[i] & 31));
+        if (list[i] >= prefix && at_word >= 0 && at_word < THREADS) atomicOr(&half[2 * at_word + (list_slot[i] >> 5 & 1)], 1u << (list_slot[i] & 31));
       }
       __syncthreads();
       if (word < words) a.stays[row * a.words + word] = word_s[tid];
@@ -438,7 +448,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
     }
     __syncthreads();
     int round_holes = 0, round_movers = 0;
-    for (int w = 0; w < kEvictWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w == wave) {
         base_s[tid] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
         if (word < words) a.ranks[row * a.words + word] = base_s[tid].x;
@@ -447,7 +457,7 @@ __global__ void __launch_bounds__(kEvictThreads) k_evict_select(EvictArgs a) {
       round_movers += (int)wave_b[w];
     }
     __syncthreads();
-    for (int w = wave; w < min(kEvictThreads, words - w0); w += kEvictWaves) {
+    for (int w = wave; w < min(THREADS, words - w0); w += WAVES) {
       const int slot0 = (w0 + w) * 64;
       const unsigned long long mask = in_scalars(word_s[w]), front = up_to(stay - slot0);
       const unsigned long long hole_mask = ~mask & up_to(length - slot0) & front, mover_mask = mask & ~front;
@@ -547,7 +557,7 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   const size_t rows = (size_t)s->batch * c->kv_heads, slots = (size_t)make_seqs(c, s).max_len;
   p.words = (int)((slots + 63) / 64);
   p.pairs = (int)(slots / 2);
-  p.parts = slots > (size_t)kKeysHere * kEvictThreads ? (int)((slots + kPartSlots - 1) / kPartSlots) : 0;
+  p.parts = slots > (size_t)kSlotsHere ? (int)((slots + kPartSlots - 1) / kPartSlots) : 0;
   p.keys = take(p.parts ? rows * slots * sizeof(uint32_t) : 0);
   p.digits = take(rows * p.parts * kDigits * sizeof(unsigned short));
   p.found = take(p.parts ? rows * sizeof(int4) : 0);
@@ -626,13 +636,15 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   rc = ctx_device(ctx);
   if (rc != STTM_OK) return rc;
   const hipStream_t s = ctx_stream(ctx);
-  const dim3 rows(a.kv_heads, seqs->batch), all(kEvictThreads);
+  const dim3 rows(a.kv_heads, seqs->batch);
   if (p.parts) {
     hipLaunchKernelGGL(k_evict_keys, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
     hipLaunchKernelGGL(k_evict_mark, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
-    hipLaunchKernelGGL((k_evict_select<0>), rows, all, 0, s, a);
-  } else {
-    hipLaunchKernelGGL((k_evict_select<kKeysHere>), rows, all, 0, s, a);
+    hipLaunchKernelGGL((k_evict_select<0, 1024>), rows, dim3(1024), 0, s, a);
+  } else if (a.seqs.max_len <= 2048) {  // (fewer wavefronts to wait for: 48 rows of 1,013 slots 10 us, by 1,024 threads 11.4)
+    hipLaunchKernelGGL((k_evict_select<8, 256>), rows, dim3(256), 0, s, a);
+  } else {                              // (128 rows of 4,097 slots 15 us, by 512 threads 17, by 256 22)
+    hipLaunchKernelGGL((k_evict_select<8, 1024>), rows, dim3(1024), 0, s, a);
   }
   const int lanes = a.pool.row <= 128 ? 8 : a.pool.row <= 256 ? 16 : a.pool.row <= 512 ? 32 : 64;
   // At most half of the slots move; some eight rows for a group of lanes.
