@@ -272,6 +272,7 @@ EVICT = [
     ("bf16", 2, 8, 64, (4097,), (4096,), 4, 64, "again", False, "zeros", "pages"),       # one goes, of many that are alike
     ("f32", 1, 8, 64, (9001, 8193), (4500, 8192), 4, 64, "again", True, "zeros", "pages"),   # rows of several workgroups
     ("bf16", 1, 8, 64, (8200, 33), (100, 5), 0, 0, "minus", False, "equal", "pages"),
+    ("bf16", 1, 8, 64, (6000,), (2500,), 3, 40, "again", False, "equal", "pages"),       # more alike than the list holds
 ]
 
 
