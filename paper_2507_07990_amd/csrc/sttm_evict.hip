@@ -22,10 +22,9 @@ struct EvictArgs {
   uint2* list;                 // [batch, kv_heads, 4096]: those (key, slot), in any order,
   int* listed;                 // [batch, kv_heads]: how many
   unsigned long long* stays;   // [batch, kv_heads, words]: a bit a slot
-  int32_t *holes, *movers;     // [batch, kv_heads, pairs]: the j-th mover goes to the j-th hole
-  int32_t* ranks;              // [batch, kv_heads, words]: holes before a word's
+  int2* ranks;                 // [batch, kv_heads, words]: holes and movers before those of a word (the j-th mover goes to the j-th hole)
   int4* counts;                // [batch, kv_heads]: pairs, new length, length, tokens so far (seqs.lengths may be lengths_out)
-  int words, pairs, parts;
+  int words, parts;
 };
 
 __device__ inline int slot_number(const EvictArgs& a, long long at, int i, int length, int total) {
@@ -206,10 +205,10 @@ __global__ void __launch_bounds__(kPartThreads) k_evict_mark(EvictArgs a) {
 // weight); the keys that share it (a few hundred to a few thousand of a long row) go on in a list in LDS, with ~number below
 // the weight; every further digit starts at the highest bit in which those left differ, so that equal weights or small numbers
 // cost no rounds of their own. It ends when the digits so far cut off exactly as many slots as stay, or 64 keys are left, which
-// one wavefront ranks. Then holes and movers are listed in the order of their slots, a word of marks a step.
+// one wavefront ranks. What is left behind is a bit a slot, and how many holes and movers come before every 64.
 //
-// Bound by the chain of counts and barriers of one workgroup: 15 us for 128 rows of 4,097 slots, 22 for four of 43,328 (6 of
-// them the lists: two stores of half a wavefront's slots for every 64).
+// Bound by the chain of counts and barriers of one workgroup: 14 us for 128 rows of 4,097 slots, 11 for four of 43,328
+// (keys and the first digit's counts ready).
 template <int KEYS, int THREADS>  // (KEYS 0 or 8)
 __global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
   constexpr bool READY = KEYS == 0;  // keys and the first digit's counts
@@ -218,7 +217,6 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
   __shared__ unsigned hist[kDigits];
   __shared__ unsigned long long list[LIST], word_s[THREADS];
   __shared__ unsigned list_slot[READY ? kListMost : 1];
-  __shared__ int2 base_s[THREADS];
   __shared__ unsigned long long few[kWave], least_s;
   __shared__ unsigned wave_a[WAVES], wave_b[WAVES], bits[4];  // bits: and, or of the keys that are left
   __shared__ int digit_s, rest_s, count_s, listed_s;
@@ -413,11 +411,10 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
         if (lane == 0) a.stays[row * a.words + (s0 >> 6)] = mask;
       });
   }
-  // Holes and movers, a round of words at a time: a thread counts a word's, then a wavefront lists a word's.
+  // How many holes and movers are before every word, a round of words at a time.
   const int words = (length + 63) / 64;
   auto up_to = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
   int holes = 0, movers = 0;
-  int32_t *hole_list = a.holes + row * a.pairs, *mover_list = a.movers + row * a.pairs;
   for (int w0 = 0; w0 < words; w0 += THREADS) {
     __syncthreads();
     const int word = w0 + tid, s0 = word * 64;
@@ -449,53 +446,84 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
     __syncthreads();
     int round_holes = 0, round_movers = 0;
     for (int w = 0; w < WAVES; ++w) {
-      if (w == wave) {
-        base_s[tid] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
-        if (word < words) a.ranks[row * a.words + word] = base_s[tid].x;
-      }
+      if (w == wave && word < words)
+        a.ranks[row * a.words + word] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
       round_holes += (int)wave_a[w];
       round_movers += (int)wave_b[w];
-    }
-    __syncthreads();
-    for (int w = wave; w < min(THREADS, words - w0); w += WAVES) {
-      const int slot0 = (w0 + w) * 64;
-      const unsigned long long mask = in_scalars(word_s[w]), front = up_to(stay - slot0);
-      const unsigned long long hole_mask = ~mask & up_to(length - slot0) & front, mover_mask = mask & ~front;
-      const int i = __builtin_amdgcn_readfirstlane(base_s[w].x) + lanes_below(hole_mask, lane);
-      const int j = __builtin_amdgcn_readfirstlane(base_s[w].y) + lanes_below(mover_mask, lane);
-      if (lane_in(hole_mask, lane) && i < a.pairs) hole_list[i] = slot0 + lane;
-      if (lane_in(mover_mask, lane) && j < a.pairs) mover_list[j] = slot0 + lane;
     }
     holes += round_holes;
     movers += round_movers;
   }
-  // (all three alike, and as many as there is room for, but for numbers that occur twice)
-  if (tid == 0) a.counts[row] = make_int4(min(min(holes, movers), a.pairs), stay, length, total);
+  // (both alike, but for numbers that occur twice)
+  if (tid == 0) a.counts[row] = make_int4(min(holes, movers), stay, length, total);
 }
 
-// A share of the tables, a slot a thread, then a share of the pairs' rows of the pool, LANES lanes a row, 16 bytes a lane. (Tables
-// and rows in workgroups of their own took 97 us where this takes 73, on the ragged batch of 24 sequences; rows through the
-// caches 102.) A mover's entries are read, written to its hole and cleared by one lane, nobody else touches either: outputs
-// may be inputs.
-constexpr int kMoveThreads = 256, kMoveRows = 4;  // (rows of a group of lanes under way together)
+// The last word in [first, end) with no more than `rank` movers before it, by a wavefront: 64 places of what is left a step.
+// (ranks[first].y is 0; the answer is the word that the mover of that rank is in.)
+__device__ inline int word_of_mover(const int2* ranks, int first, int end, int rank, int lane) {
+  while (end - first > 1) {
+    const int step = (end - first + kWave - 1) / kWave, at = first + lane * step;
+    const unsigned long long below = __ballot(at < end && ranks[min(at, end - 1)].y <= rank);
+    first += (max(1, (int)__popcll(below)) - 1) * step;
+    end = min(end, first + step);
+  }
+  return first;
+}
+
+// A workgroup has 128 slots before the new length: their entries in the tables, and the rows of the pool that go to the holes
+// among them, LANES lanes a row, 16 bytes a lane; and 128 slots behind it to clear. Its holes have consecutive ranks, so the
+// movers that fill them are consecutive too: both are listed in LDS from the marks.
+// A mover's entries are read, written to its hole and cleared by one lane, nobody else touches either: outputs may be inputs.
+// Bound by memory: 77 us for the ragged batch of 24 sequences and 8 heads (358 MB with the tables, 4.7 TB/s). 256 slots a workgroup
+// took 82 (their last rows wait alone); lists made by the search 73, but 8 more there, and 10 more for one long row, which one
+// workgroup searches. Tables and rows in workgroups of their own took 97, rows through the caches 102.
+constexpr int kMoveThreads = 256, kMoveSlots = 128, kMoveRows = 4;  // (rows of a group of lanes under way together)
 template <int LANES>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
+  __shared__ int hole_s[kMoveSlots], mover_s[kMoveSlots], span_s[2];
+  constexpr int WAVES = kMoveThreads / kWave, WORDS = kMoveSlots / kWave;  // (the first two wavefronts have a word each)
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, unit = tid & (LANES - 1);
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long row = (long long)b * a.kv_heads + h, at = row * a.slot_stride;
+  const unsigned long long* stays = a.stays + row * a.words;
+  const int2* ranks = a.ranks + row * a.words;
+  // (under way with the counts: what is past the row's words is not used)
+  const int slot0 = blockIdx.x * kMoveSlots, w0 = slot0 >> 6, word = min(w0 + wave, a.words - 1);
+  const unsigned long long mask = stays[word];
+  const int before = ranks[word].x, r0 = ranks[min(w0, a.words - 1)].x, next = ranks[min(w0 + WORDS, a.words - 1)].x;
   const int4 count = a.counts[row];
-  const int stay = count.y, length = count.z, total = count.w;
+  const int stay = count.y, length = count.z, total = count.w, words = (length + 63) / 64;
   if (blockIdx.x == 0 && h == 0 && tid == 0) a.lengths_out[b] = stay;
-  for (int i = blockIdx.x * kMoveThreads + tid; i < length; i += gridDim.x * kMoveThreads) {
-    const int bit = i & 63;
-    const unsigned long long mask = a.stays[row * a.words + (i >> 6)];
-    const bool stays = mask >> bit & 1;
-    if (i >= stay && stays) continue;  // (a mover: cleared by the slot that takes its entries)
-    int from = i >= stay ? -1 : i;     // the slot whose entries this one gets
-    if (i < stay && !stays) {
-      // (all slots of the word before this one are before the new length too)
-      const int j = a.ranks[row * a.words + (i >> 6)] + __popcll(~mask & ((1ull << bit) - 1));
-      from = j < count.x ? a.movers[row * a.pairs + j] : -1;
+  const int tail = stay + blockIdx.x * kMoveSlots + tid - kMoveSlots;
+  if (tid >= kMoveSlots && tail < length && !(stays[tail >> 6] >> (tail & 63) & 1)) {  // (movers are cleared by who takes their entries)
+    a.weights_out[at + tail] = 0.f;
+    a.ids_out[at + tail] = -1;
+    if (a.bias_out) a.bias_out[at + tail] = 0.f;
+  }
+  if (slot0 >= stay) return;
+  const int r1 = min(count.x, w0 + WORDS < words ? next : count.x), n = r1 - r0;  // n <= 128
+  // this lane's slot: it is before the new length, and it is a hole, the `place`-th of the workgroup's
+  const int slot = slot0 + tid;
+  const unsigned long long holes = ~mask & (stay - word * 64 >= 64 ? ~0ull : (1ull << max(0, stay - word * 64)) - 1);
+  const bool front = wave < WORDS && slot < stay, hole = front && lane_in(in_scalars(holes), lane);
+  const int place = before - r0 + lanes_below(holes, lane);
+  if (n > 0) {
+    if (hole && place < n) hole_s[place] = slot;
+    if (wave >= WORDS) {
+      const int w = word_of_mover(ranks, stay >> 6, words, wave == WORDS ? r0 : r1 - 1, lane);
+      if (lane == 0) span_s[wave - WORDS] = w;
     }
+    __syncthreads();
+    const int last = span_s[1];
+    for (int w = span_s[0] + wave; w <= last; w += WAVES) {
+      const unsigned long long movers = in_scalars(stays[w] & (stay - w * 64 >= 64 ? 0ull : stay - w * 64 <= 0 ? ~0ull : ~((1ull << (stay - w * 64)) - 1)));
+      const int j = ranks[w].y + lanes_below(movers, lane);
+      if (lane_in(movers, lane) && j >= r0 && j < r1) mover_s[j - r0] = w * 64 + lane;
+    }
+    __syncthreads();
+  }
+  if (front) {
+    const int from = !hole ? slot : place < n ? mover_s[place] : -1;  // the slot whose entries this one gets
     float w = 0.f, bias = 0.f;
     int id = -1;
     if (from >= 0) {
@@ -503,60 +531,57 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a) {
       id = slot_number(a, at, from, length, total);
       if (a.bias_out) bias = a.bias_in[at + from];
     }
-    a.weights_out[at + i] = w;
-    a.ids_out[at + i] = id;
-    if (a.bias_out) a.bias_out[at + i] = bias;
-    if (from > i) {
+    a.weights_out[at + slot] = w;
+    a.ids_out[at + slot] = id;
+    if (a.bias_out) a.bias_out[at + slot] = bias;
+    if (from > slot) {
       a.weights_out[at + from] = 0.f;
       a.ids_out[at + from] = -1;
       if (a.bias_out) a.bias_out[at + from] = 0.f;
     }
   }
   constexpr int GROUPS = kMoveThreads / LANES;
-  const int mask = (1 << a.pool.shift) - 1;
-  for (int j0 = blockIdx.x * GROUPS * kMoveRows + tid / LANES; j0 < count.x; j0 += gridDim.x * GROUPS * kMoveRows) {
-    int mover[kMoveRows], hole[kMoveRows], p[kMoveRows], q[kMoveRows];
+  const int page_mask = (1 << a.pool.shift) - 1;
+  const int32_t* table = a.seqs.table + b * a.seqs.table_stride;
+  for (int j0 = tid / LANES; j0 < n; j0 += GROUPS * kMoveRows) {
+    int from[kMoveRows], to[kMoveRows], p[kMoveRows], q[kMoveRows];
     uint4 k[kMoveRows], v[kMoveRows];
 #pragma unroll
     for (int r = 0; r < kMoveRows; ++r) {
-      const int j = min(j0 + r * GROUPS, count.x - 1);
-      mover[r] = a.movers[row * a.pairs + j];
-      hole[r] = a.holes[row * a.pairs + j];
+      const int j = min(j0 + r * GROUPS, n - 1);
+      from[r] = mover_s[j];
+      to[r] = hole_s[j];
+      p[r] = table[from[r] >> a.pool.shift];
+      q[r] = table[to[r] >> a.pool.shift];
     }
 #pragma unroll
     for (int r = 0; r < kMoveRows; ++r) {
-      p[r] = a.seqs.table[b * a.seqs.table_stride + (mover[r] >> a.pool.shift)];
-      q[r] = a.seqs.table[b * a.seqs.table_stride + (hole[r] >> a.pool.shift)];
-      if (p[r] < 0 || p[r] >= a.pool.pages || q[r] < 0 || q[r] >= a.pool.pages || j0 + r * GROUPS >= count.x || unit * 16 >= a.pool.row) q[r] = -1;
+      if (p[r] < 0 || p[r] >= a.pool.pages || q[r] < 0 || q[r] >= a.pool.pages || j0 + r * GROUPS >= n || unit * 16 >= a.pool.row) q[r] = -1;
+      if (q[r] < 0) continue;
+      const long long off = p[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(from[r] & page_mask) * a.pool.token_stride + unit * 16;
+      k[r] = load_once(reinterpret_cast<const uint4*>(a.pool.k + off));
+      v[r] = load_once(reinterpret_cast<const uint4*>(a.pool.v + off));
     }
 #pragma unroll
     for (int r = 0; r < kMoveRows; ++r) {
       if (q[r] < 0) continue;
-      const long long from = p[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(mover[r] & mask) * a.pool.token_stride + unit * 16;
-      k[r] = load_once(reinterpret_cast<const uint4*>(a.pool.k + from));
-      v[r] = load_once(reinterpret_cast<const uint4*>(a.pool.v + from));
-    }
-#pragma unroll
-    for (int r = 0; r < kMoveRows; ++r) {
-      if (q[r] < 0) continue;
-      const long long to = q[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(hole[r] & mask) * a.pool.token_stride + unit * 16;
-      store_once(reinterpret_cast<uint4*>(a.pool.k + to), k[r]);
-      store_once(reinterpret_cast<uint4*>(a.pool.v + to), v[r]);
+      const long long off = q[r] * a.pool.page_stride + h * a.pool.head_stride + (long long)(to[r] & page_mask) * a.pool.token_stride + unit * 16;
+      store_once(reinterpret_cast<uint4*>(a.pool.k + off), k[r]);
+      store_once(reinterpret_cast<uint4*>(a.pool.v + off), v[r]);
     }
   }
 }
 
 struct Plan {
-  int words, pairs, parts;
-  size_t keys, digits, found, list, listed, ranks, stays, holes, movers, counts, bytes;
+  int words, parts;
+  size_t keys, digits, found, list, listed, ranks, stays, counts, bytes;
 };
 Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   Plan p;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
   const size_t rows = (size_t)s->batch * c->kv_heads, slots = (size_t)make_seqs(c, s).max_len;
-  p.words = (int)((slots + 63) / 64);
-  p.pairs = (int)(slots / 2);
+  p.words = (int)std::max<size_t>(1, (slots + 63) / 64);
   p.parts = slots > (size_t)kSlotsHere ? (int)((slots + kPartSlots - 1) / kPartSlots) : 0;
   p.keys = take(p.parts ? rows * slots * sizeof(uint32_t) : 0);
   p.digits = take(rows * p.parts * kDigits * sizeof(unsigned short));
@@ -564,9 +589,7 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s) {
   p.list = take(p.parts ? rows * kListMost * sizeof(uint2) : 0);
   p.listed = take(p.parts ? rows * sizeof(int) : 0);
   p.stays = take(rows * p.words * sizeof(unsigned long long));
-  p.ranks = take(rows * p.words * sizeof(int32_t));
-  p.holes = take(rows * p.pairs * sizeof(int32_t));
-  p.movers = take(rows * p.pairs * sizeof(int32_t));
+  p.ranks = take(rows * p.words * sizeof(int2));
   p.counts = take(rows * sizeof(int4));
   p.bytes = std::max(off, (size_t)256);
   return p;
@@ -622,9 +645,7 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   a.recent = recent;
   a.keys = reinterpret_cast<uint32_t*>(ws + p.keys);
   a.stays = reinterpret_cast<unsigned long long*>(ws + p.stays);
-  a.ranks = reinterpret_cast<int32_t*>(ws + p.ranks);
-  a.holes = reinterpret_cast<int32_t*>(ws + p.holes);
-  a.movers = reinterpret_cast<int32_t*>(ws + p.movers);
+  a.ranks = reinterpret_cast<int2*>(ws + p.ranks);
   a.counts = reinterpret_cast<int4*>(ws + p.counts);
   a.digits = reinterpret_cast<unsigned short*>(ws + p.digits);
   a.found = reinterpret_cast<int4*>(ws + p.found);
@@ -632,7 +653,6 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
   a.listed = reinterpret_cast<int*>(ws + p.listed);
   a.parts = p.parts;
   a.words = p.words;
-  a.pairs = p.pairs;
   rc = ctx_device(ctx);
   if (rc != STTM_OK) return rc;
   const hipStream_t s = ctx_stream(ctx);
@@ -647,9 +667,7 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
     hipLaunchKernelGGL((k_evict_select<8, 1024>), rows, dim3(1024), 0, s, a);
   }
   const int lanes = a.pool.row <= 128 ? 8 : a.pool.row <= 256 ? 16 : a.pool.row <= 512 ? 32 : 64;
-  // At most half of the slots move; some eight rows for a group of lanes.
-  const int groups = kMoveThreads / lanes;
-  const dim3 grid(std::max(1, (p.pairs + 2 * kMoveRows * groups - 1) / (2 * kMoveRows * groups)), a.kv_heads, seqs->batch), block(kMoveThreads);
+  const dim3 grid(std::max(1, (a.seqs.max_len + kMoveSlots - 1) / kMoveSlots), a.kv_heads, seqs->batch), block(kMoveThreads);
   if (lanes == 8) hipLaunchKernelGGL((k_evict_move<8>), grid, block, 0, s, a);
   else if (lanes == 16) hipLaunchKernelGGL((k_evict_move<16>), grid, block, 0, s, a);
   else if (lanes == 32) hipLaunchKernelGGL((k_evict_move<32>), grid, block, 0, s, a);

@@ -339,6 +339,18 @@ def test_cache_evict_with_pages_outside_of_the_pool(bench):
         assert x is None or torch.equal(g.cpu(), x)
 
 
+def test_cache_evict_without_slots(bench):
+    """No pages, or no length at all: the lengths are zero, the tables are as they were."""
+    gen = _gen(14)
+    kv, table = C.pool(gen, "bf16", 2, 8, 8, (9,), junk=3.0)
+    w, keep, lens = torch.rand(1, 2, 9, generator=gen), torch.tensor([4], dtype=torch.int32), torch.tensor([0], dtype=torch.int32)
+    for t in (table, table[:, :0].clone()):
+        outs = [torch.full_like(w, 5.0), torch.full((1, 2, 9), 5, dtype=torch.int32), None]
+        got = C.run_evict(bench, kv, "pages", 8, t, lens, keep, None, 0, 0, w, None, None, *outs)
+        for g, x in zip(got, (*kv, outs[0], outs[1], None, lens)):
+            assert x is None or torch.equal(g.cpu(), x)
+
+
 def test_eviction_then_attention_over_what_stays(bench):
     """The slots that stay, in whatever order, give what attention over those tokens alone gives."""
     gen = _gen(12)
