@@ -661,9 +661,9 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
     hipLaunchKernelGGL(k_evict_keys, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
     hipLaunchKernelGGL(k_evict_mark, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
     hipLaunchKernelGGL((k_evict_select<0, 1024>), rows, dim3(1024), 0, s, a);
-  } else if (a.seqs.max_len <= 2048) {  // (fewer wavefronts to wait for: 48 rows of 1,013 slots 10 us, by 1,024 threads 11.4)
+  } else if (a.seqs.max_len <= 2048) {  // (fewer wavefronts to wait for: 48 rows of 1,013 slots 8.8 us, by 1,024 threads 10.5)
     hipLaunchKernelGGL((k_evict_select<8, 256>), rows, dim3(256), 0, s, a);
-  } else {                              // (128 rows of 4,097 slots 15 us, by 512 threads 17, by 256 22)
+  } else {                              // (128 rows of 4,097 slots 15 us where 512 threads with more keys each took 17 and 256 22, lists included)
     hipLaunchKernelGGL((k_evict_select<8, 1024>), rows, dim3(1024), 0, s, a);
   }
   const int lanes = a.pool.row <= 128 ? 8 : a.pool.row <= 256 ? 16 : a.pool.row <= 512 ? 32 : 64;
