@@ -149,7 +149,8 @@ template <int DT> __device__ inline void store_channels(char* at, const float (&
 // of one lane, one v_perm for two elements.
 //
 // P is handed on as the sum of two 16-bit numbers (16 bits of mantissa with bf16, 22 with fp16), one product each: rounding it to
-// one alone would cost as much accuracy as the result's own rounding.
+// one alone would cost as much accuracy as the result's own rounding. (The smaller number may be zero or negative, and makes NaN of
+// an infinite value: where a sum is NaN the infinite values of its channel are looked up at the end. Nothing else is spent on them.)
 //
 // Keys of the next block are loaded once this one's are used up, values likewise: no second set of registers, and there
 // are always some on their way. Two wavefronts a SIMD bound the registers to 256, which keeps the sums out of the
@@ -359,6 +360,24 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     load_values(s0 + kAttnWaves * BLOCK);
   }
 
+  // A channel's sum where it came out as NaN though no weight is: its infinite values in slots that count (their weights are above
+  // zero), if there are any.
+  auto infinite_sum = [&](int channel, float x) {
+    float sum = 0.f;
+    bool found = false;
+#pragma unroll 4
+    for (int slot = first; slot < end; ++slot) {
+      const long long at = page_at[(slot - first) >> a.pool.shift];
+      const char* value = a.pool.v + (at < 0 ? 0 : at) + (slot & page_mask) * a.pool.token_stride + channel * 2;
+      const float f = low_half<DT>(*reinterpret_cast<const unsigned short*>(value));
+      const bool masked = at < 0 || (BIAS && bias[slot] == -INFINITY);
+      if (masked || fabsf(f) < INFINITY) continue;
+      sum += f;
+      found = true;
+    }
+    return found ? sum : x;
+  };
+
   // The wavefronts' sums on a common maximum, added up in their order.
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -409,6 +428,8 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) x[e] += joined[w][(place >> 6) + 4 * e][(place & 63) + i16];
         x[e] *= share;
+        if constexpr (DT != 0)
+          if (x[e] != x[e] && total == total) x[e] = infinite_sum(channel + e, x[e]);
       }
       if (a.part) *reinterpret_cast<float4*>(a.part + (head * a.chunks + chunk) * a.d + channel) = make_float4(x[0], x[1], x[2], x[3]);
       else store_channels<DT>(a.out + b * a.out_stride + (((long long)h * a.group + head0 + i16) * a.d + channel) * ES, x);

@@ -257,6 +257,36 @@ def test_paged_attention_of_values_that_are_not_finite(bench):
     assert torch.isnan(out[0, 1]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("lengths,bias_kind", [((1, 40), ""), ((530, 33), ""), ((90, 200), "counts")])
+@pytest.mark.parametrize("d", [32, 136])
+def test_paged_attention_of_infinite_values(bench, dtype, lengths, bias_kind, d):
+    """Every weight is above zero: infinities of one sign give it, whatever the weights' last bits are; both signs or a NaN
+    give NaN; what a masked slot holds does not matter; the other channels are as they are."""
+    for seed in range(2):
+        gen = _gen(100 * d + seed)
+        kv, table = C.pool(gen, dtype, 2, d, 8, lengths)
+        bias = _bias(bias_kind, gen, (2, 2, max(lengths)))
+        if bias is not None:
+            bias[:, :, 0] = 0.0
+        for b, n in enumerate(lengths):
+            for h in range(2):
+                slots = [i for i in range(n) if bias is None or float(bias[b, h, i]) != -INF]
+                some = [slots[int(x)] for x in torch.randint(0, len(slots), (6,), generator=gen)]
+                for i, channel, value in ((some[0], 3, INF), (some[1], 8, -INF), (some[2], 17, INF), (some[3], 17, -INF), (some[4], 30, math.nan),
+                                          (some[5], 31, INF)):
+                    kv[1][int(table[b, i // 8]), h, i % 8, channel] = value
+                for i in range(n):
+                    if i not in slots:
+                        kv[1][int(table[b, i // 8]), h, i % 8] = (-INF, math.nan)[i % 2]
+        q = torch.randn(2, 6, d, generator=gen).to(TYPES[dtype])
+        lens = torch.tensor(lengths, dtype=torch.int32)
+        want = C.attention_reference(q, *kv, table, lens, 8, 0.1, bias, None, None, dtype)
+        got = C.run_attention(bench, q, kv, "pages", table, lens, 0.1, bias)
+        close(got[0], *want[0], what=f"out, seed {seed}")
+        close(got[1], *want[1], what=f"lse, seed {seed}")
+
+
 # -- eviction ----------------------------------------------------------------------------------------------------------
 
 EVICT = [
