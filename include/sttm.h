@@ -303,7 +303,8 @@ int sttm_qk_norm_rope(sttm_ctx* ctx, int dtype, int64_t n, int q_heads, int kv_h
  * key_bias, weights_in, weights_out: float [batch, kv_heads, slot_stride], slot_stride >= max_len, entries from a sequence's
  * length on neither read nor written. key_bias (or NULL): e.g. the log of the number of tokens a merged one stands for
  * (counts of sttm_reduce); -inf masks a slot, whatever its key and value hold. weights_out NULL: weights are not wanted;
- * weights_in NULL: zeros; weights_out may be weights_in. A query with no key left gets out = 0, lse = -inf and adds no weight.
+ * weights_in NULL: zeros; weights_out may be weights_in. A query with no key left gets out = 0, lse = -inf and adds no weight;
+ * a score that is NaN or +inf makes all three NaN.
  * An infinite value in a slot that counts makes its channel infinite; infinities of both signs or a NaN make it NaN (and so may an
  * infinite value whose weight is below 2^-126 of the largest, which counts as zero).
  * Sums and softmax in fp32. Results do not depend on what else runs, nor on the order of workgroups.

@@ -99,6 +99,9 @@ struct AttnArgs {
 // Softmax statistics of one head over several parts of the slots.
 __device__ inline float factor(float m, float top, float unit) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * unit); }
 
+// The logarithm of a sum of exponentials (-inf: of none; the largest s does not show a NaN, the sum does).
+__device__ inline float log_sum(float m, float total, float natural) { return m * natural + logf(total); }
+
 // A slot's elements as one lane takes them, in loads of 16 bytes (8 bytes: VW == 4 of 16 bits). ONCE: marked as used once; only
 // where rows are made of whole lines, which sixteen lanes take at a time. A lane whose share lies beyond the row takes the
 // row's start in its place: what it makes of that is not written.
@@ -396,7 +399,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   const long long head = ((long long)b * a.kv_heads + h) * a.group + head0 + i16;
   if (tid < heads) {
     if (a.stat) a.stat[head * a.chunks + chunk] = make_float2(top, total);
-    if (!a.part && a.lse) a.lse[head] = top == -INFINITY ? -INFINITY : top * a.natural + logf(total);
+    if (!a.part && a.lse) a.lse[head] = log_sum(top, total, a.natural);
   }
   const float share = a.part ? 1.f : total == 0.f ? 0.f : 1.f / total;
   if (logits && !a.stat) {  // one chunk and one tile: every slot's weight from here
@@ -588,7 +591,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
     if (tid == 0 && e < a.group) {
       const long long head = ((long long)b * a.kv_heads + h) * a.group + e;
       if (a.stat) a.stat[head * a.chunks + chunk] = make_float2(top, total);
-      if (!a.part && a.lse) a.lse[head] = top == -INFINITY ? -INFINITY : top * a.natural + logf(total);
+      if (!a.part && a.lse) a.lse[head] = log_sum(top, total, a.natural);
       all_heads[e] = make_float2(top == -INFINITY ? 0.f : top, share[e]);
     }
   }
@@ -652,7 +655,7 @@ template <int DT> __device__ inline void join_head(const AttnArgs& a, int b, int
   const int chunks = (seq_length(a.seqs, b) + a.chunk - 1) / a.chunk;
   const float2* stat = a.stat + head * a.chunks;
   const float2 all = join_stats(stat, chunks, a.unit, tid & 63);
-  if (tid == 0 && a.lse) a.lse[head] = all.x == -INFINITY ? -INFINITY : all.x * a.natural + logf(all.y);
+  if (tid == 0 && a.lse) a.lse[head] = log_sum(all.x, all.y, a.natural);
   const int units = a.d / 4, slices = kFinishThreads / units, unit = tid % units, slice = tid / units;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   if (slice < slices) {

@@ -287,6 +287,25 @@ def test_paged_attention_of_infinite_values(bench, dtype, lengths, bias_kind, d)
         close(got[1], *want[1], what=f"lse, seed {seed}")
 
 
+@pytest.mark.parametrize("dtype,q_heads,kv_heads", [("bf16", 4, 2), ("bf16", 17, 1), ("f16", 2, 2), ("f32", 2, 2), ("f32", 6, 2)])
+@pytest.mark.parametrize("n", [1, 40, 530])
+@pytest.mark.parametrize("bias_kind", ["", "lowest"])
+def test_paged_attention_of_scores_that_are_all_nan(bench, dtype, q_heads, kv_heads, n, bias_kind):
+    """NaN in the result, the weights and lse alike: -inf stands for no key left, and a part with it would be left out by who
+    joins parts. The other sequence is as it is."""
+    gen = _gen(n)
+    kv, table = C.pool(gen, dtype, kv_heads, 24, 8, (n, 9))
+    for i in range(n):
+        kv[0][int(table[0, i // 8]), :, i % 8, 2] = math.nan
+    bias = _bias(bias_kind, gen, (2, kv_heads, max(n, 9)))
+    q, lens = torch.randn(2, q_heads, 24, generator=gen).to(TYPES[dtype]), torch.tensor([n, 9], dtype=torch.int32)
+    out, lse, weights = C.run_attention(bench, q, kv, "pages", table, lens, 0.2, bias, None, torch.zeros(2, kv_heads, max(n, 9)))
+    want = C.attention_reference(q, *kv, table, lens, 8, 0.2, bias, None, torch.zeros(2, kv_heads, max(n, 9)), dtype)
+    for name, g, w in zip(("out", "lse", "weights"), (out, lse, weights), want):
+        close(g, *w, what=name)
+    assert torch.isnan(lse[0]).all() and torch.isnan(out[0]).all() and torch.isnan(weights[0, :, :n]).all() and torch.isfinite(lse[1]).all()
+
+
 # -- eviction ----------------------------------------------------------------------------------------------------------
 
 EVICT = [
