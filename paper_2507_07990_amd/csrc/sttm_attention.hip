@@ -151,8 +151,9 @@ template <int DT> __device__ inline void store_channels(char* at, const float (&
 // lanes a row): channel lane * 8 + n is row `lane` of product n. The 16-bit transposition that is left is between registers
 // of one lane, one v_perm for two elements.
 //
-// P is handed on as the sum of two 16-bit numbers (16 bits of mantissa with bf16, 22 with fp16), one product each: rounding it to
-// one alone would cost as much accuracy as the result's own rounding. (The smaller number may be zero or negative, and makes NaN of
+// P is handed on as the sum of two 16-bit numbers (16 bits of mantissa with bf16; 22 with fp16, and as 2^15 P, so that a weight is
+// off by no more than 2^-40 of the largest one where fp16 runs out of exponents), one product each: rounding it to one alone would
+// cost as much accuracy as the result's own rounding. (The smaller number may be zero or negative, and makes NaN of
 // an infinite value: where a sum is NaN the infinite values of its channel are looked up at the end. Nothing else is spent on them.)
 //
 // Keys of the next block are loaded once this one's are used up, values likewise: no second set of registers, and there
@@ -168,6 +169,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   // Values past the caches where a head's row is a number of whole lines (146 us against 155 on the ragged batch of 24
   // sequences; fp32 rows of 288 bytes took 32 against 23). Not the keys: their pieces of 64 bytes come by a line twice.
   constexpr bool ONCE = DT != 0 && PIECES != 1 && PIECES != 3 && PIECES != 6;
+  constexpr float LIFT = DT == 2 ? 15.f : 0.f;  // the largest weight is 2^LIFT while it is summed up (fp16 ends at 2^16)
   constexpr int LEAST = ES * (PIECES <= 4 ? 32 * PIECES - 24 : PIECES == 6 ? 136 : 200);
 
   __shared__ long long page_at[kChunkMax / 8];        // byte offset of every page of the chunk, -1: not in the pool
@@ -331,7 +333,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[t][r] = exp2_fast((s[t][r] - base) * a.unit);
+        p[t][r] = exp2_fast(fmaf(s[t][r] - base, a.unit, LIFT));
         l += p[t][r];
       }
     if constexpr (BIAS) clear_dead();
@@ -382,8 +384,10 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   };
 
   // The wavefronts' sums on a common maximum, added up in their order.
+  constexpr float UNLIFT = DT == 2 ? 1.f / 32768.f : 1.f;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  l *= UNLIFT;
   if (lane < kQTile) {
     stat_m[wave][lane] = m;
     stat_l[wave][lane] = l;
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   float top = stat_m[0][i16];
 #pragma unroll
   for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, stat_m[w][i16]);
-  const float mine = factor(m, top, a.unit);
+  const float mine = factor(m, top, a.unit) * UNLIFT;
   float total = 0.f;
 #pragma unroll
   for (int w = 0; w < kAttnWaves; ++w) total += stat_l[w][i16] * factor(stat_m[w][i16], top, a.unit);

@@ -306,6 +306,31 @@ def test_paged_attention_of_scores_that_are_all_nan(bench, dtype, q_heads, kv_he
     assert torch.isnan(lse[0]).all() and torch.isnan(out[0]).all() and torch.isnan(weights[0, :, :n]).all() and torch.isfinite(lse[1]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n", [200, 700])
+def test_paged_attention_of_many_small_weights(bench, dtype, n):
+    """Weights far below the largest one count together: one key of a high score whose value is zero, and slots of 2^-20 to
+    2^-34 of its weight with large values, which alone make up the result. Tolerance: a weight's own rounding (scores of up to
+    24: 24 * 20 e; two numbers of 16 bits: at least 15 bits together), and the result's."""
+    gen = _gen(n)
+    kv, table = C.pool(gen, dtype, 1, 16, 8, (n,))
+    q = torch.zeros(1, 2, 16)
+    q[0, 0, 0], q[0, 1, 0] = 1.0, 0.75
+    small = torch.rand(n, generator=gen) * 1.4
+    for i in range(n):
+        at = int(table[0, i // 8]), 0, i % 8
+        kv[0][at], kv[1][at] = 0.0, 30000.0
+        kv[0][at][0] = small[i]
+    top = n // 3
+    kv[0][int(table[0, top // 8]), 0, top % 8, 0] = 24.0
+    kv[1][int(table[0, top // 8]), 0, top % 8] = 0.0
+    q, lens = q.to(TYPES[dtype]), torch.tensor([n], dtype=torch.int32)
+    want = C.attention_reference(q, *kv, table, lens, 8, 1.0, None, None, None, dtype)[0][0]
+    got = C.run_attention(bench, q, kv, "pages", table, lens, 1.0)[0]
+    assert float(want.min()) > 1e-4      # (above the smallest normal fp16 number)
+    close(got, want, want * (24 * 20 * C.E + 2.0 ** -15 + n * C.E + U[dtype] * 1.1) + 2.0 ** -25, what="out")
+
+
 # -- eviction ----------------------------------------------------------------------------------------------------------
 
 EVICT = [
