@@ -10,7 +10,7 @@ namespace {
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kQTile = 16;      // heads of a group that one matrix product takes
 constexpr int kChunkMax = 512;  // slots of one workgroup at most
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 typedef float f32x4 __attribute__((vector_size(16)));
 typedef uint32_t u32x4 __attribute__((vector_size(16)));
@@ -86,21 +86,19 @@ struct AttnArgs {
   const float *bias, *weights_in;
   float *weights_out, *lse;
   long long slot_stride;
-  float* logits;     // [batch, kv_heads, max_len, group]: s_j in the units below (weights wanted), else NULL
+  float* logits;     // [batch, kv_heads, max_len, group]: s_j (weights wanted), else NULL
   float* part;       // [batch, q_heads, chunks, d]: unnormalised sums of the chunks (more than one chunk), else NULL
   float2* stat;      // [batch, q_heads, chunks]: largest s and sum of exponentials of a chunk
-  float scale;       // of the product q.k: with unit = 1 the caller's times log2(e)
-  float natural;     // a unit of s, in natural logarithms: ln(2) or 1
-  float unit;        // s * unit is an exponent of two: 1, or log2(e) with a bias (s is then left as it is, since the lowest
-                     // fp32 number as a bias has no multiple)
+  float scale;
   int kv_heads, group, d, chunk, chunks, tiles;
 };
 
-// Softmax statistics of one head over several parts of the slots.
-__device__ inline float factor(float m, float top, float unit) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * unit); }
+// Softmax statistics of one head over several parts of the slots. (s is kept as it is and differences are multiplied by log2(e): s
+// itself may be the lowest fp32 number, or near the largest, and has no multiple then.)
+__device__ inline float factor(float m, float top) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * kLog2e); }
 
 // The logarithm of a sum of exponentials (-inf: of none; the largest s does not show a NaN, the sum does).
-__device__ inline float log_sum(float m, float total, float natural) { return m * natural + logf(total); }
+__device__ inline float log_sum(float m, float total) { return m + logf(total); }
 
 // A slot's elements as one lane takes them, in loads of 16 bytes (8 bytes: VW == 4 of 16 bits). ONCE: marked as used once; only
 // where rows are made of whole lines, which sixteen lanes take at a time. A lane whose share lies beyond the row takes the
@@ -319,7 +317,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     top = fmaxf(top, __shfl_xor(top, 16, 64));
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     if (__ballot(top > m) != 0) {  // (seldom after the first blocks)
-      const float m2 = fmaxf(m, top), shrink = factor(m, m2, a.unit);
+      const float m2 = fmaxf(m, top), shrink = factor(m, m2);
       m = m2;
       l *= shrink;
 #pragma unroll
@@ -333,7 +331,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[t][r] = exp2_fast(fmaf(s[t][r] - base, a.unit, LIFT));
+        p[t][r] = exp2_fast(fmaf(s[t][r] - base, kLog2e, LIFT));
         l += p[t][r];
       }
     if constexpr (BIAS) clear_dead();
@@ -396,14 +394,14 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
   float top = stat_m[0][i16];
 #pragma unroll
   for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, stat_m[w][i16]);
-  const float mine = factor(m, top, a.unit) * UNLIFT;
+  const float mine = factor(m, top) * UNLIFT;
   float total = 0.f;
 #pragma unroll
-  for (int w = 0; w < kAttnWaves; ++w) total += stat_l[w][i16] * factor(stat_m[w][i16], top, a.unit);
+  for (int w = 0; w < kAttnWaves; ++w) total += stat_l[w][i16] * factor(stat_m[w][i16], top);
   const long long head = ((long long)b * a.kv_heads + h) * a.group + head0 + i16;
   if (tid < heads) {
     if (a.stat) a.stat[head * a.chunks + chunk] = make_float2(top, total);
-    if (!a.part && a.lse) a.lse[head] = log_sum(top, total, a.natural);
+    if (!a.part && a.lse) a.lse[head] = log_sum(top, total);
   }
   const float share = a.part ? 1.f : total == 0.f ? 0.f : 1.f / total;
   if (logits && !a.stat) {  // one chunk and one tile: every slot's weight from here
@@ -412,7 +410,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     const long long slots = ((long long)b * a.kv_heads + h) * a.slot_stride;
     for (int slot = tid; slot < end; slot += kAttnThreads) {
       float sum = 0.f;
-      for (int i = 0; i < heads; ++i) sum = fmaf(exp2_fast((logits[(long long)slot * a.group + i] - all_heads[i].x) * a.unit), all_heads[i].y, sum);
+      for (int i = 0; i < heads; ++i) sum = fmaf(exp2_fast((logits[(long long)slot * a.group + i] - all_heads[i].x) * kLog2e), all_heads[i].y, sum);
       a.weights_out[slots + slot] = (a.weights_in ? a.weights_in[slots + slot] : 0.f) + sum;
     }
   }
@@ -544,7 +542,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) top = fmaxf(top, s[e][r]);
       if (__ballot(top > m[e]) != 0) {  // (seldom after the first blocks)
-        const float shrink = factor(m[e], top, a.unit);
+        const float shrink = factor(m[e], top);
         m[e] = top;
         l[e] *= shrink;
 #pragma unroll
@@ -553,7 +551,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
       const float base = m[e] == -INFINITY ? 0.f : m[e];
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        p[e][r] = exp2_fast((s[e][r] - base) * a.unit);
+        p[e][r] = exp2_fast((s[e][r] - base) * kLog2e);
         l[e] += p[e][r];
       }
     }
@@ -582,8 +580,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
   for (int e = 0; e < HEADS; ++e) {
     float top = -INFINITY, total = 0.f;
     for (int w = 0; w < 4 * kAttnWaves; ++w) top = fmaxf(top, stat_m[w][e]);
-    for (int w = 0; w < 4 * kAttnWaves; ++w) total += stat_l[w][e] * factor(stat_m[w][e], top, a.unit);
-    const float mine = factor(m[e], top, a.unit);
+    for (int w = 0; w < 4 * kAttnWaves; ++w) total += stat_l[w][e] * factor(stat_m[w][e], top);
+    const float mine = factor(m[e], top);
 #pragma unroll
     for (int n = 0; n < VW; ++n) {
       float x = acc[e][n] * mine;
@@ -595,7 +593,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
     if (tid == 0 && e < a.group) {
       const long long head = ((long long)b * a.kv_heads + h) * a.group + e;
       if (a.stat) a.stat[head * a.chunks + chunk] = make_float2(top, total);
-      if (!a.part && a.lse) a.lse[head] = log_sum(top, total, a.natural);
+      if (!a.part && a.lse) a.lse[head] = log_sum(top, total);
       all_heads[e] = make_float2(top == -INFINITY ? 0.f : top, share[e]);
     }
   }
@@ -604,7 +602,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
     const long long slots = ((long long)b * a.kv_heads + h) * a.slot_stride;
     for (int slot = tid; slot < end; slot += kAttnThreads) {
       float sum = 0.f;
-      for (int e = 0; e < a.group; ++e) sum = fmaf(exp2_fast((logits[(long long)slot * a.group + e] - all_heads[e].x) * a.unit), all_heads[e].y, sum);
+      for (int e = 0; e < a.group; ++e) sum = fmaf(exp2_fast((logits[(long long)slot * a.group + e] - all_heads[e].x) * kLog2e), all_heads[e].y, sum);
       a.weights_out[slots + slot] = (a.weights_in ? a.weights_in[slots + slot] : 0.f) + sum;
     }
   }
@@ -625,7 +623,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) k_paged_attention_rows(AttnAr
 }
 
 // Maximum and sum of one head over its chunks, the same in all lanes of a wavefront.
-__device__ inline float2 join_stats(const float2* stat, int chunks, float unit, int lane) {
+__device__ inline float2 join_stats(const float2* stat, int chunks, int lane) {
   float top = -INFINITY, total = 0.f;
   for (int c0 = 0; c0 < chunks; c0 += 4 * kWave) {
     float2 x[4];
@@ -637,15 +635,15 @@ __device__ inline float2 join_stats(const float2* stat, int chunks, float unit, 
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) most = fmaxf(most, x[k].x);
-    total *= factor(top, most, unit);
+    total *= factor(top, most);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) total = fmaf(x[k].y, factor(x[k].x, most, unit), total);
+    for (int k = 0; k < 4; ++k) total = fmaf(x[k].y, factor(x[k].x, most), total);
     top = most;
   }
   float all = top;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-  return make_float2(all, wave_sum(total * factor(top, all, unit)));
+  return make_float2(all, wave_sum(total * factor(top, all)));
 }
 
 constexpr int kFinishThreads = 256;
@@ -658,8 +656,8 @@ template <int DT> __device__ inline void join_head(const AttnArgs& a, int b, int
   const long long head = (long long)b * a.kv_heads * a.group + h;
   const int chunks = (seq_length(a.seqs, b) + a.chunk - 1) / a.chunk;
   const float2* stat = a.stat + head * a.chunks;
-  const float2 all = join_stats(stat, chunks, a.unit, tid & 63);
-  if (tid == 0 && a.lse) a.lse[head] = log_sum(all.x, all.y, a.natural);
+  const float2 all = join_stats(stat, chunks, tid & 63);
+  if (tid == 0 && a.lse) a.lse[head] = log_sum(all.x, all.y);
   const int units = a.d / 4, slices = kFinishThreads / units, unit = tid % units, slice = tid / units;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   if (slice < slices) {
@@ -667,7 +665,7 @@ template <int DT> __device__ inline void join_head(const AttnArgs& a, int b, int
 #pragma unroll 8
     for (int c = slice; c < chunks; c += slices) {
       const float4 y = *reinterpret_cast<const float4*>(part + (long long)c * a.d);
-      const float f = factor(stat[c].x, all.x, a.unit);
+      const float f = factor(stat[c].x, all.x);
       x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
     }
   }
@@ -698,15 +696,15 @@ __device__ inline void add_weights(const AttnArgs& a, int b, int h, int first, f
   for (int q = 0; q < AHEAD; ++q) ahead[q] = x[min(q, a.group - 1)];
   if (a.weights_in) before = a.weights_in[at];
   for (int q = tid / kWave; q < a.group; q += kFinishThreads / kWave) {
-    const float2 r = join_stats(a.stat + (row * a.group + q) * a.chunks, chunks, a.unit, tid & 63);
+    const float2 r = join_stats(a.stat + (row * a.group + q) * a.chunks, chunks, tid & 63);
     if ((tid & 63) == 0) of_head[q] = make_float2(r.x == -INFINITY ? 0.f : r.x, r.y == 0.f ? 0.f : 1.f / r.y);
   }
   __syncthreads();
   float sum = 0.f;
 #pragma unroll
   for (int q = 0; q < AHEAD; ++q)
-    if (q < a.group) sum = fmaf(exp2_fast((ahead[q] - of_head[q].x) * a.unit), of_head[q].y, sum);
-  for (int q = AHEAD; q < a.group; ++q) sum = fmaf(exp2_fast((x[q] - of_head[q].x) * a.unit), of_head[q].y, sum);
+    if (q < a.group) sum = fmaf(exp2_fast((ahead[q] - of_head[q].x) * kLog2e), of_head[q].y, sum);
+  for (int q = AHEAD; q < a.group; ++q) sum = fmaf(exp2_fast((x[q] - of_head[q].x) * kLog2e), of_head[q].y, sum);
   if (first + tid < length) a.weights_out[at] = before + sum;
 }
 
@@ -839,9 +837,7 @@ extern "C" int sttm_paged_attention(sttm_ctx* ctx, const sttm_cache* cache, cons
   if (weights_out) a.logits = reinterpret_cast<float*>(ws + p.logits);
   if (p.chunks > 1) a.part = reinterpret_cast<float*>(ws + p.part);
   if (p.chunks > 1 || (weights_out && !p.whole)) a.stat = reinterpret_cast<float2*>(ws + p.stat);
-  a.unit = key_bias ? kLog2e : 1.f;
-  a.natural = key_bias ? 1.f : kLn2;
-  a.scale = key_bias ? scale : scale * kLog2e;
+  a.scale = scale;
   a.kv_heads = cache->kv_heads;
   a.group = q_heads / cache->kv_heads;
   a.d = cache->head_dim;

@@ -331,6 +331,30 @@ def test_paged_attention_of_many_small_weights(bench, dtype, n):
     close(got, want, want * (24 * 20 * C.E + 2.0 ** -15 + n * C.E + U[dtype] * 1.1) + 2.0 ** -25, what="out")
 
 
+@pytest.mark.parametrize("dtype,heads", [("bf16", 2), ("f16", 2), ("f32", 1), ("f32", 3)])
+@pytest.mark.parametrize("n", [20, 530])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_paged_attention_of_scores_near_the_largest_number(bench, dtype, heads, n, with_bias):
+    """Scores of 3e38, 0 and -3e38 are finite numbers of 32 bits: the first ones share the weight."""
+    gen = _gen(n)
+    kv, table = C.pool(gen, dtype, 1, 8, 8, (n,))
+    for i in range(n):
+        kv[0][int(table[0, i // 8]), 0, i % 8] = 0.0
+        kv[0][int(table[0, i // 8]), 0, i % 8, 0] = (0.0, 1.0, -1.0)[i % 3]
+    q = torch.zeros(1, heads, 8)
+    q[:, :, 0] = 1.0
+    q, lens, bias = q.to(TYPES[dtype]), torch.tensor([n], dtype=torch.int32), torch.zeros(1, 1, n) if with_bias else None
+    zero = torch.zeros(1, 1, n)
+    want = C.attention_reference(q, *kv, table, lens, 8, 3e38, bias, None, zero, dtype)
+    got = C.run_attention(bench, q, kv, "pages", table, lens, 3e38, bias, None, zero)
+    some = torch.arange(n) % 3 == 1
+    even = torch.stack([kv[1][int(table[0, i // 8]), 0, i % 8] for i in range(n) if i % 3 == 1]).double().mean(0)
+    assert torch.allclose(want[0][0][0, 0], even)
+    for name, g, w in zip(("out", "lse", "weights"), got, want):
+        close(g, w[0], {"out": 2 * U[dtype] * 4.0, "lse": 1e32, "weights": 1e-5}[name], what=name)
+    assert (got[2].cpu()[0, 0][~some] == 0).all()
+
+
 # -- eviction ----------------------------------------------------------------------------------------------------------
 
 EVICT = [
