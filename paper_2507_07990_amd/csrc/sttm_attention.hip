@@ -754,7 +754,7 @@ int check_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences
   if (rc != STTM_OK) return rc;
   if (q_heads < 1 || q_heads % cache->kv_heads || q_heads / cache->kv_heads > 256 || q_heads > 65535)
     return ctx_fail(ctx, STTM_ERR_SHAPE, "need q_heads a multiple of kv_heads, at most 256 a kv head, q_heads <= 65535");
-  if ((double)seqs->batch * q_heads * seqs->max_len > 1e14) return ctx_fail(ctx, STTM_ERR_SHAPE, "batch * q_heads * max_len too large");
+  if ((double)seqs->batch * q_heads * make_seqs(cache, seqs).max_len > 1e14) return ctx_fail(ctx, STTM_ERR_SHAPE, "batch * q_heads * max_len too large");
   return STTM_OK;
 }
 

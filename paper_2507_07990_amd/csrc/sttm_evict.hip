@@ -599,7 +599,7 @@ int check_evict(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* se
   int rc = check_cache(ctx, cache);
   if (rc == STTM_OK) rc = check_sequences(ctx, cache, seqs);
   if (rc != STTM_OK) return rc;
-  if ((double)seqs->batch * cache->kv_heads * seqs->max_len > 1e13) return ctx_fail(ctx, STTM_ERR_SHAPE, "batch * kv_heads * max_len too large");
+  if ((double)seqs->batch * cache->kv_heads * make_seqs(cache, seqs).max_len > 1e13) return ctx_fail(ctx, STTM_ERR_SHAPE, "batch * kv_heads * max_len too large");
   return STTM_OK;
 }
 

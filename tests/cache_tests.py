@@ -561,3 +561,28 @@ def test_nothing_to_do(bench):
     ctx.sttm_paged_attention(z(0, 4, 16), cache, seqs, z(0, 4, 16), 1.0)
     n = z(0, dtype=torch.int32)
     ctx.sttm_cache_evict(cache, seqs, n, n, z(0, 2, 16), z(0, 2, 16), None, z(0, 2, 16, dtype=torch.int32))
+
+
+def test_large_batches_without_a_max_len(bench):
+    """Without max_len a sequence ends with its row of the table, and that is what counts in the limits of a call."""
+    lib, ctx = bench.lib, bench.ctx
+    z = lambda *s, dtype=torch.float32: bench.put(torch.zeros(*s, dtype=dtype))   # noqa: E731
+    batch, H, K = 1500, 64, 8
+    cache = lib.PagedCache(z(2, K, 8, 8), z(2, K, 8, 8))
+    table = torch.ones(batch, 1, dtype=torch.int32)
+    seqs = lib.Sequences(bench.put(table), z(batch, dtype=torch.int32))
+    assert lib.sttm_paged_attention_workspace_bytes(cache, seqs, H, True) > 0 and lib.sttm_cache_evict_workspace_bytes(cache, seqs) > 0
+    w, ids, n = z(batch, K, 8), z(batch, K, 8, dtype=torch.int32), z(batch, dtype=torch.int32)
+    _refused(bench, lib.STTM_ERR_WORKSPACE, ctx.sttm_paged_attention, z(batch, H, 8), cache, seqs, z(batch, H, 8), 1.0)   # (the last thing asked for)
+    _refused(bench, lib.STTM_ERR_WORKSPACE, ctx.sttm_cache_evict, cache, seqs, n, n, w, w, ids, ids)
+
+
+def test_refusals_of_what_is_too_large(bench):
+    """Described only: refused before anything is read."""
+    lib, ctx = bench.lib, bench.ctx
+    z = lambda *s, dtype=torch.float32: bench.put(torch.zeros(*s, dtype=dtype))   # noqa: E731
+    cache, q = lib.PagedCache(z(2, 8, 8, 8), z(2, 8, 8, 8)), z(1, 64, 8)
+    seqs = lib.Sequences(z(1, 2, dtype=torch.int32), z(1, dtype=torch.int32))
+    seqs.struct.batch, seqs.struct.max_pages, seqs.struct.table_stride = 60000, 1 << 26, 1 << 26
+    assert lib.sttm_paged_attention_workspace_bytes(cache, seqs, 64, True) == 0 and lib.sttm_cache_evict_workspace_bytes(cache, seqs) == 0
+    _refused(bench, lib.STTM_ERR_SHAPE, ctx.sttm_paged_attention, q, cache, seqs, q, 1.0)
