@@ -258,8 +258,9 @@ typedef struct {
 /* The sequences of a batch: slot i of sequence b is slot i % page_size of page block_table[b*table_stride + i/page_size].
  * max_len: no length is above it (launches are sized by it; a length above it, or above the pages of a row, is read as if
  * it were that, one below zero as zero). Entries of the table behind a sequence's last slot are not read. A page number
- * outside the pool is not followed: its slots count as masked. batch <= 65535 (0: nothing is done). With n the lesser of
- * max_len and max_pages * page_size: batch * q_heads * n <= 1e14 (attention), batch * kv_heads * n <= 1e13 (eviction). */
+ * outside the pool is not followed: its slots count as masked. batch <= 65535 (0: nothing is done). max_pages * page_size
+ * < 2^31; with n the lesser of max_len and max_pages * page_size: n <= 2^30, batch * q_heads * n <= 1e14 (attention),
+ * batch * kv_heads * n <= 1e13 (eviction). */
 typedef struct {
   const int32_t* block_table; /* device [batch, max_pages] */
   const int32_t* lengths;     /* device [batch] */

@@ -28,6 +28,8 @@ int check_sequences(sttm_ctx* c, const sttm_cache* p, const sttm_sequences* s) {
   if (s->batch < 0 || s->batch > 65535 || s->max_pages < 0 || s->max_len < 0 || s->table_stride < s->max_pages)
     return ctx_fail(c, STTM_ERR_SHAPE, "need 0 <= batch <= 65535, max_pages >= 0, max_len >= 0, table_stride >= max_pages");
   if ((int64_t)s->max_pages * p->page_size >= (1ll << 31)) return ctx_fail(c, STTM_ERR_SHAPE, "need max_pages * page_size < 2^31");
+  // (slots are numbered in 32 bits, and the numbers run on by up to as many: behind the new length, past the end in whole blocks)
+  if (make_seqs(p, s).max_len > 1 << 30) return ctx_fail(c, STTM_ERR_SHAPE, "need no more than 2^30 slots a sequence (max_len, or max_pages * page_size)");
   if (s->batch && (!s->lengths || (!s->block_table && s->max_pages && s->max_len)))
     return ctx_fail(c, STTM_ERR_NULL, "block_table or lengths is NULL");
   return STTM_OK;

@@ -586,3 +586,21 @@ def test_refusals_of_what_is_too_large(bench):
     seqs.struct.batch, seqs.struct.max_pages, seqs.struct.table_stride = 60000, 1 << 26, 1 << 26
     assert lib.sttm_paged_attention_workspace_bytes(cache, seqs, 64, True) == 0 and lib.sttm_cache_evict_workspace_bytes(cache, seqs) == 0
     _refused(bench, lib.STTM_ERR_SHAPE, ctx.sttm_paged_attention, q, cache, seqs, q, 1.0)
+
+
+def test_refusals_of_sequences_that_slot_numbers_do_not_reach(bench):
+    """Slots are numbered in 32 bits, twice as many as a sequence may have: 2^30 are the most. Described only."""
+    lib, ctx = bench.lib, bench.ctx
+    z = lambda *s, dtype=torch.float32: bench.put(torch.zeros(*s, dtype=dtype))   # noqa: E731
+    cache, q = lib.PagedCache(z(2, 1, 8, 8), z(2, 1, 8, 8)), z(1, 1, 8)
+    seqs = lib.Sequences(z(1, 2, dtype=torch.int32), z(1, dtype=torch.int32))
+    t, i = z(1, 1, 16), z(1, 1, 16, dtype=torch.int32)
+    n = z(1, dtype=torch.int32)
+    for pages, max_len, ok in ((1 << 27, 2 ** 31 - 1, True), ((1 << 27) + 1, 2 ** 31 - 1, False), ((1 << 28) - 1, 1 << 30, True),
+                               ((1 << 28) - 1, (1 << 30) + 1, False), (2, 2 ** 31 - 1, True)):
+        seqs.struct.max_pages, seqs.struct.table_stride, seqs.struct.max_len = pages, pages, max_len
+        sizes = [lib.sttm_paged_attention_workspace_bytes(cache, seqs, 1, True), lib.sttm_cache_evict_workspace_bytes(cache, seqs)]
+        assert (min(sizes) > 0) == ok and (max(sizes) > 0) == ok
+        if not ok:
+            _refused(bench, lib.STTM_ERR_SHAPE, ctx.sttm_paged_attention, q, cache, seqs, q, 1.0)
+            _refused(bench, lib.STTM_ERR_SHAPE, ctx.sttm_cache_evict, cache, seqs, n, n, t, t, i, i)
