@@ -330,8 +330,8 @@ size_t sttm_paged_attention_workspace_bytes(const sttm_cache* cache, const sttm_
  * Tables: float weights_in/out and bias_in/out (bias both or neither NULL), int32 ids_in/out (ids_in NULL: all below zero),
  * all [batch, kv_heads, slot_stride]; an output may be its input. Outputs: the tokens that stay, with their numbers; from the
  * new length to the old one weight 0, number -1, bias 0; behind that as they were. lengths_out int32 [batch] (may be
- * the lengths of seqs). No number may occur twice in one (sequence, kv head) (which of them stay is open then). Pages that several sequences share must
- * not be among those that change. A slot whose page number lies outside the
+ * the lengths of seqs). No number should occur twice in one (sequence, kv head): which of its slots stay is open
+ * then, and nothing else. Pages that several sequences share must not be among those that change. A slot whose page number lies outside the
  * pool takes part in the order; its rows are not moved.
  * workspace as for sttm_paged_attention, of sttm_cache_evict_workspace_bytes(...) bytes. Asynchronous. */
 int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* seqs, const int32_t* keep_dev,

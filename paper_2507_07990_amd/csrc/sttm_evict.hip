@@ -325,9 +325,12 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
         __syncthreads();
         if (wave == 0) {
           const unsigned long long mine = lane < count ? few[lane] : 0;
-          int above = 0;
-          for (int i = 0; i < count; ++i) above += few[i] >= mine;
-          if (lane < count && above == left) least_s = mine;
+          int above = 0, over = 0;
+          for (int i = 0; i < count; ++i) {
+            above += few[i] >= mine;
+            over += few[i] > mine;
+          }
+          if (lane < count && over < left && above >= left) least_s = mine;  // (one lane's, but for numbers that occur twice)
         }
         __syncthreads();
         prefix = least_s;
@@ -414,47 +417,67 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(EvictArgs a) {
   // How many holes and movers are before every word, a round of words at a time.
   const int words = (length + 63) / 64;
   auto up_to = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
-  int holes = 0, movers = 0;
-  for (int w0 = 0; w0 < words; w0 += THREADS) {
-    __syncthreads();
-    const int word = w0 + tid, s0 = word * 64;
-    if (word < words) word_s[tid] = a.stays[row * a.words + word];
-    __syncthreads();
-    if (in_list && marked) {
-      unsigned* half = reinterpret_cast<unsigned*>(word_s);
-      for (int i = tid; i < listed; i += THREADS) {
-        const int at_word = (int)(list_slot[i] >> 6) - w0;
-        if (list[i] >= prefix && at_word >= 0 && at_word < THREADS) atomicOr(&half[2 * at_word + (list_slot[i] >> 5 & 1)], 1u << (list_slot[i] & 31));
+  bool to_mark = in_list && marked;
+  int holes, movers;
+  for (int pass = 0; pass < 2; ++pass) {
+    holes = movers = 0;
+    for (int w0 = 0; w0 < words; w0 += THREADS) {
+      __syncthreads();
+      const int word = w0 + tid, s0 = word * 64;
+      if (word < words) word_s[tid] = a.stays[row * a.words + word];
+      __syncthreads();
+      if (to_mark) {
+        unsigned* half = reinterpret_cast<unsigned*>(word_s);
+        for (int i = tid; i < listed; i += THREADS) {
+          const int at_word = (int)(list_slot[i] >> 6) - w0;
+          if (list[i] >= prefix && at_word >= 0 && at_word < THREADS) atomicOr(&half[2 * at_word + (list_slot[i] >> 5 & 1)], 1u << (list_slot[i] & 31));
+        }
+        __syncthreads();
+        if (word < words) a.stays[row * a.words + word] = word_s[tid];
+      }
+      unsigned long long hole = 0, mover = 0;
+      if (word < words) {
+        const unsigned long long mask = word_s[tid], front = up_to(stay - s0);
+        hole = ~mask & up_to(length - s0) & front;
+        mover = mask & ~front;
+      }
+      unsigned my_hole = (unsigned)__popcll(hole), my_mover = (unsigned)__popcll(mover);
+      const unsigned own_hole = my_hole, own_mover = my_mover;
+      my_hole = wave_inclusive(my_hole, lane);
+      my_mover = wave_inclusive(my_mover, lane);
+      if (lane == 63) {
+        wave_a[wave] = my_hole;
+        wave_b[wave] = my_mover;
       }
       __syncthreads();
-      if (word < words) a.stays[row * a.words + word] = word_s[tid];
+      int round_holes = 0, round_movers = 0;
+      for (int w = 0; w < WAVES; ++w) {
+        if (w == wave && word < words)
+          a.ranks[row * a.words + word] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
+        round_holes += (int)wave_a[w];
+        round_movers += (int)wave_b[w];
+      }
+      holes += round_holes;
+      movers += round_movers;
     }
-    unsigned long long hole = 0, mover = 0;
-    if (word < words) {
-      const unsigned long long mask = word_s[tid], front = up_to(stay - s0);
-      hole = ~mask & up_to(length - s0) & front;
-      mover = mask & ~front;
+    if (movers <= holes) break;
+    // A number that occurs twice is the last one that stays, with all its slots: those that are too many go, the first ones.
+    to_mark = false;
+    if (tid == 0) listed_s = movers - holes;
+    for (int w = 0; w < WAVES; ++w) {  // (one wavefront after the other: the same ones on every call)
+      __syncthreads();
+      if (w != wave) continue;
+      int surplus = listed_s;
+      each(true, [&](int s0, int, bool there, uint32_t k, int id) {
+        const bool same = there && whole_key(k, id) == prefix;
+        const int before = lanes_below(__ballot(same), lane);
+        const unsigned long long gone = __ballot(same && before < surplus);
+        if (lane == 0 && gone) a.stays[row * a.words + (s0 >> 6)] &= ~gone;
+        surplus -= (int)__popcll(gone);
+      });
+      if (lane == 0) listed_s = surplus;
     }
-    unsigned my_hole = (unsigned)__popcll(hole), my_mover = (unsigned)__popcll(mover);
-    const unsigned own_hole = my_hole, own_mover = my_mover;
-    my_hole = wave_inclusive(my_hole, lane);
-    my_mover = wave_inclusive(my_mover, lane);
-    if (lane == 63) {
-      wave_a[wave] = my_hole;
-      wave_b[wave] = my_mover;
-    }
-    __syncthreads();
-    int round_holes = 0, round_movers = 0;
-    for (int w = 0; w < WAVES; ++w) {
-      if (w == wave && word < words)
-        a.ranks[row * a.words + word] = make_int2(holes + round_holes + (int)(my_hole - own_hole), movers + round_movers + (int)(my_mover - own_mover));
-      round_holes += (int)wave_a[w];
-      round_movers += (int)wave_b[w];
-    }
-    holes += round_holes;
-    movers += round_movers;
   }
-  // (both alike, but for numbers that occur twice)
   if (tid == 0) a.counts[row] = make_int4(min(holes, movers), stay, length, total);
 }
 

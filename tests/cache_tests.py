@@ -423,6 +423,32 @@ def test_cache_evict_of_numbers_that_occur_twice(bench):
     assert got[5].tolist() == [keep] and (got[3][0, 0, :keep] == 7).sum() <= keep
 
 
+@pytest.mark.parametrize("n,keep", [(60, 31), (300, 121), (1100, 1099), (5000, 2501), (9001, 101), (9001, 8999)])
+@pytest.mark.parametrize("times,w_kind", [(2, "equal"), (5, "equal"), (3, "ties")])
+def test_cache_evict_leaves_whole_tables_where_numbers_occur_twice(bench, n, keep, times, w_kind):
+    """Which of the slots of one number stay is open. Everything else is as ever: the other numbers that stay, every token with
+    its own row and weight, no slot twice, and nothing left behind the new length."""
+    gen = _gen(n + times)
+    kv, table = C.pool(gen, "f32", 1, 8, 64, (n,), junk=-5.0)
+    perm = torch.randperm(n, generator=gen)
+    ids = torch.zeros(1, 1, n, dtype=torch.int32)
+    ids[0, 0, perm] = (torch.arange(n) // times).to(torch.int32)
+    w = torch.full((1, 1, n), 0.5) if w_kind == "equal" else (ids % 3).float()     # (alike where the numbers are)
+    for i in range(n):
+        kv[0][int(table[0, i // 64]), 0, i % 64], kv[1][int(table[0, i // 64]), 0, i % 64] = float(i), -float(i)
+    lens, keeps = torch.tensor([n], dtype=torch.int32), torch.tensor([keep], dtype=torch.int32)
+    outs = [torch.full_like(w, 9.0), torch.full_like(ids, 9), None]
+    k, v, w2, ids2, _, new = [x if x is None else x.cpu() for x in
+                              C.run_evict(bench, kv, "pages", 8, table, lens, keeps, None, 0, 0, w, ids, None, *outs)]
+    assert new.tolist() == [keep]
+    want = sorted(range(n), key=lambda i: (-float(w[0, 0, i]), int(ids[0, 0, i])))[:keep]
+    assert sorted(ids2[0, 0, :keep].tolist()) == sorted(ids[0, 0, want].tolist())
+    fro = torch.stack([k[int(table[0, i // 64]), 0, i % 64, 0] for i in range(keep)]).long()
+    assert len(set(fro.tolist())) == keep and torch.equal(ids[0, 0, fro], ids2[0, 0, :keep]) and torch.equal(w[0, 0, fro], w2[0, 0, :keep])
+    assert torch.equal(torch.stack([v[int(table[0, i // 64]), 0, i % 64, 0] for i in range(keep)]).long(), -fro)
+    assert (ids2[0, 0, keep:] == -1).all() and (w2[0, 0, keep:] == 0).all()
+
+
 def test_cache_evict_with_pages_outside_of_the_pool(bench):
     """Their slots take part in the order; rows are neither read from nor written to them."""
     gen = _gen(11)
