@@ -322,8 +322,9 @@ size_t sttm_paged_attention_workspace_bytes(const sttm_cache* cache, const sttm_
 /* Eviction by accumulated weight. Every slot of a (sequence, kv head) holds a token with a number: ids_in[slot], or where
  * that is below zero total - length + slot (tokens appended one after the other since the last eviction; total int32
  * [batch]: how many tokens the sequence has had, NULL = its length). keep int32 [batch] (device): the new length is
- * min(length, max(keep, 0)). The slots that stay are the first ones in this order: numbers below `sink` or from
- * total - recent on before all others; then the larger weights_in (NaN behind all numbers); then the lower number.
+ * min(length, max(keep, 0)). The slots that stay are the first ones in this order: those with numbers below `sink` or from
+ * total - recent on, whatever their weights, the lower number first (a keep below sink + recent leaves the lowest of these numbers
+ * and none of the newest); then all others, the larger weights_in first (NaN behind all numbers), of equal ones the lower number.
  * The slots that stay but lie behind the new length move, in ascending order, into the slots before it whose tokens went,
  * ascending: rows of k and v in the pool, and the entries of the tables. (Keys carry their positions, so that
  * attention does not depend on the order of slots; as few rows move as can.) The pages behind the new length are free then.

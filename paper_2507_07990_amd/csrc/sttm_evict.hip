@@ -32,7 +32,7 @@ __device__ inline int slot_number(const EvictArgs& a, long long at, int i, int l
   return id < 0 ? total - length + i : id;
 }
 
-// The order of the slots: larger ones stay, equal ones by the lower number. Protected slots are above all weights, NaN
+// The order of the slots: larger ones stay, equal ones by the lower number. Protected slots are above all weights and all alike, NaN
 // below (float_key has numbers in 0x007fffff .. 0xff800000); both zeros are alike.
 __device__ inline uint32_t weight_key(float w, int id, int total, const EvictArgs& a) {
   if (id < a.sink || (long long)id >= (long long)total - a.recent) return 0xffffffffu;

@@ -449,6 +449,17 @@ def test_cache_evict_leaves_whole_tables_where_numbers_occur_twice(bench, n, kee
     assert (ids2[0, 0, keep:] == -1).all() and (w2[0, 0, keep:] == 0).all()
 
 
+def test_cache_evict_among_protected_slots_goes_by_their_numbers(bench):
+    """Fewer stay than are protected: the lowest numbers do, whatever the weights."""
+    gen, n = _gen(15), 100
+    kv, table = C.pool(gen, "f32", 1, 8, 8, (n,), junk=3.0)
+    w = torch.arange(n).float()[None, None].clone()
+    lens, keep = torch.tensor([n], dtype=torch.int32), torch.tensor([12], dtype=torch.int32)
+    ids = C.run_evict(bench, kv, "pages", 8, table, lens, keep, None, 4, 32, w, None, None, torch.zeros_like(w), torch.zeros(1, 1, n, dtype=torch.int32),
+                      None)[3].cpu()
+    assert sorted(ids[0, 0, :12].tolist()) == [0, 1, 2, 3, 68, 69, 70, 71, 72, 73, 74, 75]
+
+
 def test_cache_evict_with_pages_outside_of_the_pool(bench):
     """Their slots take part in the order; rows are neither read from nor written to them."""
     gen = _gen(11)
