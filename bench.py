@@ -33,8 +33,9 @@ def source_digest() -> str:
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2507_07990_amd", "csrc")
+    cache = ("sttm_cache.h", "sttm_rope.hip", "sttm_attention.hip", "sttm_evict.hip")
     for name in sorted(os.listdir(csrc)):
-        if name in ("sttm_api.hip", "sttm_dev.h", "sttm_reduce.hip", "sttm_spatial.hip", "sttm_temporal.hip"):
+        if name.endswith((".hip", ".h")) and name not in cache:
             h.update(name.encode())
             h.update(open(os.path.join(csrc, name), "rb").read())
     return h.hexdigest()
