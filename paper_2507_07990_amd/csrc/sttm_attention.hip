@@ -9,7 +9,11 @@ namespace {
 
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kQTile = 16;      // heads of a group that one matrix product takes
-constexpr int kChunkMax = 512;  // slots of one workgroup at most
+// Slots of one workgroup at most. (A host-thread build of the tests sets fewer, for many chunks of short sequences.)
+#ifndef STTM_CHUNK_MAX
+#define STTM_CHUNK_MAX 512
+#endif
+constexpr int kChunkMax = STTM_CHUNK_MAX, kChunkMid = kChunkMax / 2, kChunkLeast = kChunkMax / 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef float f32x4 __attribute__((vector_size(16)));
@@ -735,7 +739,7 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s, int q_heads, bool w
   // have several of unequal sequences (the batch 142 us, by 256 153, by 1,024 148; one sequence of 43,328 slots by 256 21); of
   // 128 only where 256 would leave compute units without any (that sequence by 128: 24).
   const long long rows = (long long)std::max(s->batch, 1) * c->kv_heads * p.tiles, len = std::max(max_len, 1);
-  p.chunk = len <= kChunkMax || rows * len >= kChunkMax * 4096ll ? kChunkMax : rows * len >= 256 * 256ll ? 256 : 128;
+  p.chunk = len <= kChunkMax || rows * len >= kChunkMax * 4096ll ? kChunkMax : rows * len >= kChunkMid * 256ll ? kChunkMid : kChunkLeast;
   p.chunks = (int)((len + p.chunk - 1) / p.chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };

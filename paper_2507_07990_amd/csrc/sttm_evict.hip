@@ -59,9 +59,14 @@ __device__ inline int lanes_below(unsigned long long mask, int lane) {
 }
 
 constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
-constexpr int kListMost = 4096;                            // keys that fit the list in LDS
-constexpr int kPartThreads = 256, kPartSlots = 4096;       // of one workgroup that works out keys
-constexpr int kSlotsHere = 8192;                           // rows up to here are gone through by one workgroup alone
+// Keys that fit the list in LDS; slots of one workgroup that works out keys; rows up to here are gone through by one workgroup
+// alone. (A host-thread build of the tests sets fewer: short rows take the way of long ones.)
+#ifndef STTM_EVICT_LIST
+#define STTM_EVICT_LIST 4096
+#define STTM_EVICT_PART 4096
+#define STTM_EVICT_HERE 8192
+#endif
+constexpr int kListMost = STTM_EVICT_LIST, kPartSlots = STTM_EVICT_PART, kSlotsHere = STTM_EVICT_HERE, kPartThreads = 256;
 
 // GROUP keys of a lane, 64 slots apart from `from` on; all loads under way together.
 template <int GROUP>

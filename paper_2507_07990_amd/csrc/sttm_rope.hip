@@ -132,9 +132,15 @@ template <int DT> struct Run {
 };
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeWaves = 2048;          // two a SIMD; more of them work the angles out more often (4,915 tokens by 4,915 wavefronts
-                                          // 35 us, by 9,830 40)
-constexpr int64_t kOnceBytes = 32 << 20;  // the eight L2 of the card together
+// Wavefronts: two a SIMD; more of them work the angles out more often (4,915 tokens by 4,915 wavefronts 35 us, by 9,830 40). Bytes
+// that the eight L2 of the card hold together. (A host-thread build of the tests sets 1 and 0: a wavefront has many rows of heads,
+// which go past the caches.)
+#ifndef STTM_ROPE_WAVES
+#define STTM_ROPE_WAVES 2048
+#define STTM_ROPE_ONCE_BYTES (32 << 20)
+#endif
+constexpr int kRopeWaves = STTM_ROPE_WAVES;
+constexpr int64_t kOnceBytes = STTM_ROPE_ONCE_BYTES;
 
 // LANES lanes share a head's row, eight channels a lane: the two runs of four that its four pairs consist of (or eight
 // channels in a row where pairs are neighbours, and behind the rotated part). A wavefront has 64 / LANES rows of the same

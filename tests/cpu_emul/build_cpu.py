@@ -28,7 +28,7 @@ def _up_to_date(out):
     if not os.path.exists(out):
         return False
     folders = [CSRC, os.path.join(ROOT, "include"), HERE, os.path.join(HERE, "hip")]
-    files = [os.path.join(d, f) for d in folders for f in os.listdir(d) if f.endswith((".h", ".hip", ".cpp", "build_cpu.py"))]
+    files = [os.path.join(d, f) for d in folders for f in os.listdir(d) if f.endswith((".h", ".hip", ".cpp", "build_cpu.py", "build_cache_cpu.py"))]
     return os.path.getmtime(out) > max(map(os.path.getmtime, files))
 
 
