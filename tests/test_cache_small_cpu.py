@@ -2,6 +2,7 @@
 chunks (more than a wavefront joins in one go), evictions by many workgroups with a list that holds few slots, wavefronts that
 have many rows of heads and write past the caches."""
 import ctypes
+import os
 import shutil
 
 import pytest
@@ -17,7 +18,7 @@ def bench():
     from paper_2507_07990_amd import binding
     from tests.cpu_emul import build_cache_cpu
     real = binding._lib
-    binding._lib = binding._declare(ctypes.CDLL(build_cache_cpu.build(small=True)))
+    binding._lib = binding._declare(ctypes.CDLL(build_cache_cpu.build_sanitized() if "STTM_SANITIZED" in os.environ else build_cache_cpu.build(small=True)))
     try:
         ctx = binding.Sttm(0, stream_ptr=0)
         ctx._device_index = -1                  # (host tensors)
