@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[t][r] = exp2_fast(fmaf(s[t][r] - base, kLog2e, LIFT));
+        p[t][r] = exp2_fast(DT == 2 ? fmaf(s[t][r] - base, kLog2e, LIFT) : (s[t][r] - base) * kLog2e);
         l += p[t][r];
       }
     if constexpr (BIAS) clear_dead();
@@ -367,22 +367,22 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
     load_values(s0 + kAttnWaves * BLOCK);
   }
 
-  // A channel's sum where it came out as NaN though no weight is: its infinite values in slots that count (their weights are above
-  // zero), if there are any.
-  auto infinite_sum = [&](int channel, float x) {
-    float sum = 0.f;
-    bool found = false;
-#pragma unroll 4
+  // Four channels' sums, some of them NaN though no weight is: those get their infinite values in slots that count (whose weights are
+  // above zero), if they have any. (One short loop out of the way: code that is seldom run, unrolled in place, cost every call 0.5 us.)
+  auto look_up_infinite = [&](int channel, float (&x)[4]) {
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
     for (int slot = first; slot < end; ++slot) {
       const long long at = page_at[(slot - first) >> a.pool.shift];
-      const char* value = a.pool.v + (at < 0 ? 0 : at) + (slot & page_mask) * a.pool.token_stride + channel * 2;
-      const float f = low_half<DT>(*reinterpret_cast<const unsigned short*>(value));
+      const uint2 v4 = *reinterpret_cast<const uint2*>(a.pool.v + (at < 0 ? 0 : at) + (slot & page_mask) * a.pool.token_stride + channel * 2);
+      const float f[4] = {low_half<DT>(v4.x), high_half<DT>(v4.x), low_half<DT>(v4.y), high_half<DT>(v4.y)};
       const bool masked = at < 0 || (BIAS && bias[slot] == -INFINITY);
-      if (masked || fabsf(f) < INFINITY) continue;
-      sum += f;
-      found = true;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += masked || fabsf(f[e]) < INFINITY ? 0.f : f[e];
     }
-    return found ? sum : x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (x[e] != x[e] && sum[e] != 0.f) x[e] = sum[e];
   };
 
   // The wavefronts' sums on a common maximum, added up in their order.
@@ -437,8 +437,10 @@ __global__ void __launch_bounds__(kAttnThreads, VW == 16 ? 1 : 2) k_paged_attent
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) x[e] += joined[w][(place >> 6) + 4 * e][(place & 63) + i16];
         x[e] *= share;
-        if constexpr (DT != 0)
-          if (x[e] != x[e] && total == total) x[e] = infinite_sum(channel + e, x[e]);
+      }
+      if constexpr (DT != 0) {
+        const float all = (x[0] + x[1]) + (x[2] + x[3]);
+        if (__builtin_expect(all != all && total == total, 0)) look_up_infinite(channel, x);
       }
       if (a.part) *reinterpret_cast<float4*>(a.part + (head * a.chunks + chunk) * a.d + channel) = make_float4(x[0], x[1], x[2], x[3]);
       else store_channels<DT>(a.out + b * a.out_stride + (((long long)h * a.group + head0 + i16) * a.d + channel) * ES, x);
