@@ -309,14 +309,16 @@ int sttm_qk_norm_rope(sttm_ctx* ctx, int dtype, int64_t n, int q_heads, int kv_h
  * a score that is NaN or +inf makes all three NaN.
  * An infinite value in a slot that counts makes its channel infinite; infinities of both signs or a NaN make it NaN (and so may an
  * infinite value whose weight is below 2^-126 of the largest, which counts as zero).
- * Sums and softmax in fp32. Results do not depend on what else runs, nor on the order of workgroups.
+ * Sums and softmax in fp32, values summed up before the division: |v| times the length has to stay in fp32's range. Results do
+ * not depend on what else runs, nor on the order of workgroups.
  * workspace: sttm_paged_attention_workspace_bytes(...) bytes on the device, 256-byte aligned, overwritten at will; calls that
  * overlap in time need one each. Asynchronous. */
 int sttm_paged_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* seqs, int q_heads, float scale,
                          const void* q_dev, int64_t q_stride, const float* key_bias_dev, const float* weights_in_dev,
                          float* weights_out_dev, int64_t slot_stride, void* out_dev, int64_t out_stride, float* lse_dev,
                          void* workspace_dev, size_t workspace_bytes);
-/* Bytes for a call with weights_out (weights != 0) or without; 0 for descriptions that a call would refuse. */
+/* Bytes for a call with weights_out (weights != 0) or without; 0 for descriptions that a call would refuse. (For these
+ * descriptions: fewer slots may be cut into more chunks, and need more.) */
 size_t sttm_paged_attention_workspace_bytes(const sttm_cache* cache, const sttm_sequences* seqs, int q_heads, int weights);
 
 /* Eviction by accumulated weight. Every slot of a (sequence, kv head) holds a token with a number: ids_in[slot], or where

@@ -159,8 +159,9 @@ template <int DT> __device__ inline void store_channels(char* at, const float (&
 // an infinite value: where a sum is NaN the infinite values of its channel are looked up at the end. Nothing else is spent on them.)
 //
 // Keys of the next block are loaded once this one's are used up, values likewise: no second set of registers, and there
-// are always some on their way. Two wavefronts a SIMD bound the registers to 256, which keeps the sums out of the
-// accumulation registers that only copies reach.
+// are always some on their way. Up to 128 channels two wavefronts a SIMD bound the registers to 256, which keeps the sums out of
+// the accumulation registers that only copies reach. Above, one wavefront a SIMD has them there in part (8 sequences of 16,384 slots,
+// 4 kv heads of 256 channels: bf16 137 us, bound to 256 registers 139; fp32 226 and 310; but bf16 heads of 192 119 and 93).
 //
 // Bound by memory: 24 sequences of 901 to 25,977 slots, 64 heads on 8 of 128 bf16 channels, are 760 MB in 142 us (5.3 TB/s; the
 // matrix units are busy a twentieth of the time); one of 43,328 slots, 28 heads on 4, with scores kept, 90 MB in 21 us.
@@ -736,10 +737,15 @@ Plan make_plan(const sttm_cache* c, const sttm_sequences* s, int q_heads, bool w
   Plan p;
   const int group = q_heads / c->kv_heads, max_len = make_seqs(c, s).max_len;
   p.tiles = (group + kQTile - 1) / kQTile;
-  // One chunk for short sequences: a second launch costs more than the few blocks that follow each other (257 slots 8.1 us, as
-  // three chunks 9.7). Else chunks of 256 or 512 slots, the longer ones where there are enough of them for every compute unit to
-  // have several of unequal sequences (the batch 142 us, by 256 153, by 1,024 148; one sequence of 43,328 slots by 256 21); of
-  // 128 only where 256 would leave compute units without any (that sequence by 128: 24).
+  // One chunk for short sequences: a second launch costs more than the few blocks that follow each other (in a graph, 4 kv heads of
+  // 128 bf16 channels: 257 slots 8.6 us, as three chunks 9.6; 64 sequences of 512 slots 17 and 24. One sequence alone would gain
+  // from 400 slots on, 512: 12 and 9.7, and with weights from 257 on, 11.7 and 10.2). Else chunks of 256 or 512 slots, the longer ones where there are enough of them for every compute unit to
+  // have several of unequal sequences (the batch 142 us, by 256 153, by 1,024 148; one sequence of 43,328 slots by 256 21);
+  // of 128 only where 256 would leave compute units without any (that sequence by 128: 24).
+  // Whole calls in a graph, bf16 heads of 128 channels, by 128 / 256 / 512 slots, us: 4,096 slots in all rows 10.1 / 12.0 / 15.7;
+  // 32,768 12.5 / 14.4 / 17.5; 65,536 16.2 / 15.2 / 18.4; 131,072 24.8 / 21.4 / 20.6; 262,144 41 / 36 / 32; 524,288 69 / 61 / 57;
+  // 1,048,576 128 / 111 / 99; 2,097,152 246 / 212 / 192. fp32 rows of 72, 398,320 slots: 49.6 / 49.8 / 52.3; 2,097,152: 217 / 213 / 209.
+  // (So between the two bounds 512 is up to a tenth faster for 16-bit rows, and 256 for short fp32 ones.)
   const long long rows = (long long)std::max(s->batch, 1) * c->kv_heads * p.tiles, len = std::max(max_len, 1);
   p.chunk = len <= kChunkMax || rows * len >= kChunkMax * 4096ll ? kChunkMax : rows * len >= kChunkMid * 256ll ? kChunkMid : kChunkLeast;
   p.chunks = (int)((len + p.chunk - 1) / p.chunk);

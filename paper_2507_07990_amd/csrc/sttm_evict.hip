@@ -59,8 +59,9 @@ __device__ inline int lanes_below(unsigned long long mask, int lane) {
 }
 
 constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
-// Keys that fit the list in LDS; slots of one workgroup that works out keys; rows up to here are gone through by one workgroup
-// alone. (A host-thread build of the tests sets fewer: short rows take the way of long ones.)
+// Keys that fit the list in LDS; slots of one workgroup that works out keys; rows up to here, as many as the registers of one
+// workgroup hold, are gone through by it alone (whole calls in a graph, one slot going: four rows of 2,300 slots 12 us, as long rows
+// 18; of 8,192 15 and 19; 128 of 8,192 24 and 31; 512 of them 55 and 61). (A host-thread build of the tests sets fewer: short rows take the way of long ones.)
 #ifndef STTM_EVICT_LIST
 #define STTM_EVICT_LIST 4096
 #define STTM_EVICT_PART 4096
@@ -99,7 +100,7 @@ __device__ inline void count_digit(unsigned* hist, bool mine, uint32_t digit, in
 }
 
 // Long rows: keys and the counts of their first digit, a workgroup for every kPartSlots slots, so that a few long rows are
-// gone through by many compute units (four rows of 43,328 slots: 7 us here and 9 in k_evict_mark, where one workgroup a row took
+// gone through by many compute units (four rows of 43,328 slots: 6 us here and 9 in k_evict_mark, where one workgroup a row took
 // 40 for as much; parts of 2,048 slots 5 and 10, and 8 and 16 against 9 and 11 on 192 ragged rows).
 __global__ void __launch_bounds__(kPartThreads) k_evict_keys(EvictArgs a) {
   __shared__ unsigned hist[kDigits];
@@ -689,9 +690,11 @@ extern "C" int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const st
     hipLaunchKernelGGL(k_evict_keys, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
     hipLaunchKernelGGL(k_evict_mark, dim3(p.parts, a.kv_heads, seqs->batch), dim3(kPartThreads), 0, s, a);
     hipLaunchKernelGGL((k_evict_select<0, 1024>), rows, dim3(1024), 0, s, a);
-  } else if (a.seqs.max_len <= 2048) {  // (fewer wavefronts to wait for: 48 rows of 1,013 slots 8.8 us, by 1,024 threads 10.5)
+  } else if (a.seqs.max_len <= 2048) {  // (as many slots as their registers hold. Fewer wavefronts to wait for: whole calls in a graph,
+                                        // 48 rows of 500 slots 10.8 us, by 1,024 threads 12.1; of 1,013 11.1 and 13.2; of 2,048
+                                        // 12.1 and 13.8; 512 rows of 2,048 22 and 31)
     hipLaunchKernelGGL((k_evict_select<8, 256>), rows, dim3(256), 0, s, a);
-  } else {                              // (128 rows of 4,097 slots 15 us where 512 threads with more keys each took 17 and 256 22, lists included)
+  } else {                              // (128 rows of 4,097 slots 14 us; 512 threads with twice the keys each took 2 more, 256 7 more)
     hipLaunchKernelGGL((k_evict_select<8, 1024>), rows, dim3(1024), 0, s, a);
   }
   const int lanes = a.pool.row <= 128 ? 8 : a.pool.row <= 256 ? 16 : a.pool.row <= 512 ? 32 : 64;

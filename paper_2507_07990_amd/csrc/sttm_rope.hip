@@ -147,7 +147,8 @@ constexpr int64_t kOnceBytes = STTM_ROPE_ONCE_BYTES;
 // token side by side, so that cos and sin of a lane's pairs serve all heads it comes by.
 // The angle is position * frequency in turns, in 64 bits, where whole turns are taken off exactly: in 32 bits position 43,264
 // would leave an angle 2^-9 off.
-// Bound by memory: 43,264 tokens of 28 + 4 heads of 128 bf16 channels are 798 MB in 156 us, 5.1 TB/s, the rate of a copy. ONCE:
+// Bound by memory: 43,264 tokens of 28 + 4 heads of 128 bf16 channels are 798 MB in 155 us where launches follow each other,
+// 5.1 TB/s, the rate of a copy (in the first ones after idle up to 169). ONCE:
 // what is written is more than the caches are good for and goes past them (4,915 fp32 tokens 28 us against 36).
 template <int DT, int LANES, bool ONCE>
 __global__ void __launch_bounds__(kRopeThreads) k_qk_norm_rope(RopeArgs a) {
