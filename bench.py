@@ -29,11 +29,12 @@ HBM_PEAK_GBS = 8000.0
 
 def source_digest() -> str:
     """sha256 over the sources of the merge path: a traffic figure is only quoted for the code it was measured on. (The
-    operators on a paged cache, which this script does not run, are other files.)"""
+    operators for a model behind the merge, which this script does not run, are other files.)"""
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2507_07990_amd", "csrc")
-    cache = ("sttm_cache.h", "sttm_rope.hip", "sttm_attention.hip", "sttm_evict.hip")
+    cache = ("sttm_cache.h", "sttm_rope.hip", "sttm_attention.hip", "sttm_evict.hip", "sttm_queries.h", "sttm_queries_kernel.h",
+             "sttm_queries.hip", "sttm_queries_f32.hip", "sttm_queries_bf16.hip", "sttm_queries_f16.hip", "sttm_residual.hip")
     for name in sorted(os.listdir(csrc)):
         if name.endswith((".hip", ".h")) and name not in cache:
             h.update(name.encode())

@@ -343,6 +343,65 @@ int sttm_cache_evict(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequence
                      float* bias_out_dev, int32_t* lengths_out_dev, void* workspace_dev, size_t workspace_bytes);
 size_t sttm_cache_evict_workspace_bytes(const sttm_cache* cache, const sttm_sequences* seqs);
 
+/* ---- several queries, and what stands around attention in a layer --------------------------------------------------- */
+
+/* As the calls on a paged cache, these work on the caller's buffers alone, can be called in any order and in a stream capture, allocate
+ * nothing, copy nothing and never synchronise.
+ *
+ * Queries. q, out [tokens, q_heads, d] (rows q_stride / out_stride elements apart, 16-byte aligned, the heads of a row one after the
+ * other); q_heads is a multiple of kv_heads, head h reads key-value head h / (q_heads / kv_heads), q_heads / kv_heads <= 256. The tokens of
+ * sequence b are the rows q_offsets[b] .. q_offsets[b + 1] - 1 (device int64 [batch + 1], ascending; NULL: one token for each sequence,
+ * tokens == batch). Rows in front of the first sequence and behind the last one are neither read nor written. tokens <= 2^22, tokens *
+ * q_heads / kv_heads <= 2^28. lse float [tokens, q_heads] (may be NULL) = log sum_j exp(s_j) over the keys that a query sees.
+ * Scores and sums are held in fp32; a softmax weight is rounded to 16 bits before it meets a 16-bit value (fp16: as 2^15 times itself),
+ * the result once more. A query with no key left gets out = 0, lse = -inf; a score that is NaN or +inf makes both NaN. An infinite value in a
+ * slot that counts makes its channel infinite; infinities of both signs or a NaN make it NaN (and so may an infinite value whose weight is below
+ * 2^-126 of the largest, fp16 2^-40, which counts as zero); what stands in a key or value that a query does not see does not matter. Values are
+ * summed up before the division: |v| times the number of keys has to stay in fp32's range. Results do not depend on what else runs, nor on the order
+ * of workgroups.
+ * workspace: ..._workspace_bytes(...) bytes on the device, 256-byte aligned, overwritten at will; calls that overlap in time need
+ * one each. */
+
+/* The states of a batch, one sequence after the other: the row of head h of state r starts at element r*row_stride + h*head_stride of k
+ * and of v and has head_dim elements (two parts of one projection's output will do). Sequence b has the rows offsets[b] ..
+ * offsets[b + 1] - 1 (device int64 [batch + 1], ascending, e.g. the offsets of sttm_reduce), no more than max_rows of them (launches
+ * are sized by it; rows behind it are not read, nor any behind `rows`). head_dim % 8 == 0, 8 <= head_dim <= 256; 1 <= kv_heads <= 1024; k, v and strides
+ * multiples of 16 bytes; max_rows <= 2^30; batch <= 65535. */
+typedef struct {
+  const void* k; /* device */
+  const void* v; /* device */
+  int dtype;     /* sttm_dtype of the rows */
+  int kv_heads, head_dim;
+  int64_t rows, row_stride, head_stride;
+  const int64_t* offsets; /* device */
+  int batch, max_rows;
+} sttm_states;
+
+/* Attention of every sequence's tokens over all states of the same sequence, whatever the two lengths are. s_j = scale * (q . k_j) +
+ * key_bias of state j: float [rows] (bias_stride 0) or [kv_heads, rows] with rows of heads bias_stride elements apart, or NULL; e.g. the log of the
+ * number of tokens a merged one stands for; -inf masks a state. Asynchronous. */
+int sttm_cross_attention(sttm_ctx* ctx, const sttm_states* states, int64_t tokens, int q_heads, float scale, const void* q_dev,
+                         int64_t q_stride, const int64_t* q_offsets_dev, const float* key_bias_dev, int64_t bias_stride, void* out_dev,
+                         int64_t out_stride, float* lse_dev, void* workspace_dev, size_t workspace_bytes);
+/* 0 for descriptions that a call would refuse. (For these numbers: fewer tokens may be cut into more parts, and need more.) */
+size_t sttm_cross_attention_workspace_bytes(const sttm_states* states, int64_t tokens, int q_heads);
+
+/* Attention of the newest tokens of sequences that go on from shared prefixes, on a paged cache. prefixes: one entry for each group
+ * (block tables and lengths of the slots that a group shares); group g has the sequences group_offsets[g] .. group_offsets[g + 1] - 1
+ * (device int32 [groups + 1], ascending; a sequence of no group has no prefix). prefixes NULL: none. seqs: each sequence's own slots, which
+ * follow the prefix; the keys and values of its n tokens are its last n own slots already, and token j of them sees the prefix and the
+ * own slots before length - (n - 1 - j). A prefix's keys and values are read once for all tokens of its group.
+ * prefix_bias float [groups, kv_heads, prefix_slots], key_bias float [batch, kv_heads, key_slots] (either may be NULL; entries from a
+ * length on are not read): added to the scores, -inf masks a slot. As for sttm_paged_attention a page number outside the pool masks
+ * its slots. Asynchronous. */
+int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* prefixes, const int32_t* group_offsets_dev,
+                          const sttm_sequences* seqs, int64_t tokens, int q_heads, float scale, const void* q_dev, int64_t q_stride,
+                          const int64_t* q_offsets_dev, const float* prefix_bias_dev, int64_t prefix_slots, const float* key_bias_dev,
+                          int64_t key_slots, void* out_dev, int64_t out_stride, float* lse_dev, void* workspace_dev,
+                          size_t workspace_bytes);
+size_t sttm_shared_attention_workspace_bytes(const sttm_cache* cache, const sttm_sequences* prefixes, const sttm_sequences* seqs,
+                                             int64_t tokens, int q_heads);
+
 /* ---- inspection ---------------------------------------------------------------------------------------- */
 
 /* Copies an internal table (device to device, asynchronous) into dst_dev; bytes must equal the table's size. */

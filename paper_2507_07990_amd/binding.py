@@ -31,7 +31,8 @@ EXPORTS = [
     "sttm_profile_enable", "sttm_profile_read", "sttm_set_match_mode", "sttm_set_output_order", "sttm_positions",
     "sttm_set_cell_dots", "sttm_invalidate", "sttm_reduce_noalloc", "sttm_reduce_noalloc_max_bytes",
     "sttm_reduce_noalloc_bytes", "sttm_qk_norm_rope", "sttm_paged_attention", "sttm_paged_attention_workspace_bytes",
-    "sttm_cache_evict", "sttm_cache_evict_workspace_bytes",
+    "sttm_cache_evict", "sttm_cache_evict_workspace_bytes", "sttm_cross_attention", "sttm_cross_attention_workspace_bytes",
+    "sttm_shared_attention", "sttm_shared_attention_workspace_bytes",
 ]
 STTM_MATCH_FIRST_PASSING, STTM_MATCH_TOPLEFT_ONLY, STTM_MATCH_MOST_SIMILAR = 0, 1, 2
 STTM_ORDER_RASTER, STTM_ORDER_ZSCAN = 0, 1
@@ -55,6 +56,13 @@ class _RopeStruct(C.Structure):
     """sttm_rope"""
     _fields_ = [("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("pos_stride", C.c_int64), ("sections", C.c_int * 3),
                 ("pos_float", C.c_int), ("interleaved", C.c_int)]
+
+
+class _StatesStruct(C.Structure):
+    """sttm_states"""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("rows", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("offsets", C.c_void_p),
+                ("batch", C.c_int), ("max_rows", C.c_int)]
 
 
 def _load() -> C.CDLL:
@@ -103,6 +111,13 @@ def _declare(lib: C.CDLL) -> C.CDLL:
     lib.sttm_cache_evict.argtypes = [vp, cache, seqs, vp, vp, i, i, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz]
     lib.sttm_cache_evict_workspace_bytes.argtypes = [cache, seqs]
     lib.sttm_cache_evict_workspace_bytes.restype = sz
+    states = C.POINTER(_StatesStruct)
+    lib.sttm_cross_attention.argtypes = [vp, states, i64, i, f, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz]
+    lib.sttm_cross_attention_workspace_bytes.argtypes = [states, i64, i]
+    lib.sttm_cross_attention_workspace_bytes.restype = sz
+    lib.sttm_shared_attention.argtypes = [vp, cache, seqs, vp, seqs, i64, i, f, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz]
+    lib.sttm_shared_attention_workspace_bytes.argtypes = [cache, seqs, seqs, i64, i]
+    lib.sttm_shared_attention_workspace_bytes.restype = sz
     return lib
 
 
@@ -201,6 +216,38 @@ class Rope:
         self.struct = _RopeStruct(_ptr(positions), _ptr(inv_freq), stride, (C.c_int * 3)(*parts, *[0] * (3 - len(parts))),
                                   int(positions.dtype == torch.float32), int(interleaved))
         self.ref = C.byref(self.struct)
+
+
+class States:
+    """sttm_states: keys and values of a batch, tensors [rows, kv_heads, head_dim] of one type and one set of strides (the last one 1;
+    e.g. two parts of one projection's output), sequence b from row offsets[b] on (int64 [batch + 1]); no sequence has more than
+    max_rows (default: all rows)."""
+
+    def __init__(self, k, v, offsets, max_rows: Optional[int] = None):
+        _expect(k.dim() == 3 and k.shape == v.shape and k.stride() == v.stride() and k.stride(2) == 1, STTM_ERR_SHAPE,
+                "k and v must be [rows, kv_heads, head_dim] with the same strides, the last one 1")
+        _expect(k.dtype == v.dtype and k.dtype in _DTYPES, STTM_ERR_DTYPE, "k and v must be of one type, float32, bfloat16 or float16")
+        _expect(offsets.dtype == torch.int64, STTM_ERR_DTYPE, "offsets must be int64")
+        _expect(offsets.dim() == 1 and offsets.numel() >= 1 and offsets.is_contiguous(), STTM_ERR_SHAPE, "offsets must be [batch + 1], contiguous")
+        _expect(k.device == v.device == offsets.device, STTM_ERR_ARG, "k, v and offsets must be on one device")
+        _expect(max_rows is None or max_rows >= 0, STTM_ERR_SHAPE, "max_rows must not be negative")
+        self.k, self.v, self.offsets, self.dtype, self.device = k, v, offsets, k.dtype, k.get_device()
+        self.rows, self.kv_heads, self.head_dim = k.shape
+        self.batch = offsets.numel() - 1
+        self.max_rows = self.rows if max_rows is None else min(int(max_rows), self.rows)
+        strides = [st if n > 1 else 0 for n, st in zip(k.shape, k.stride())]   # (the stride of a single entry means nothing)
+        self.struct = _StatesStruct(_ptr(k), _ptr(v), _DTYPES[k.dtype], self.kv_heads, self.head_dim, self.rows, strides[0], strides[1],
+                                    _ptr(offsets), self.batch, min(self.max_rows, 2**31 - 1))
+        self.ref = C.byref(self.struct)
+
+
+def sttm_cross_attention_workspace_bytes(states: States, tokens: int, q_heads: int) -> int:
+    return int(_lib.sttm_cross_attention_workspace_bytes(states.struct, tokens, q_heads))
+
+
+def sttm_shared_attention_workspace_bytes(cache: PagedCache, prefixes: Optional[Sequences], sequences: Sequences, tokens: int, q_heads: int) -> int:
+    return int(_lib.sttm_shared_attention_workspace_bytes(cache.struct, prefixes.struct if prefixes is not None else None, sequences.struct,
+                                                          tokens, q_heads))
 
 
 def sttm_paged_attention_workspace_bytes(cache: PagedCache, sequences: Sequences, q_heads: int, weights: bool = False) -> int:
@@ -442,6 +489,64 @@ class Sttm:
                                    _table(ids_in, "ids_in", i32, shape, dev), _table(ids_out, "ids_out", i32, shape, dev),
                                    _table(bias_in, "bias_in", f32, shape, dev), _table(bias_out, "bias_out", f32, shape, dev),
                                    _vector(lengths_out, "lengths_out", i32, batch, dev), ws, size)
+        if rc != STTM_OK:
+            self._check(rc)
+
+    # -- several queries ---------------------------------------------------------------------------------
+    def _queries(self, q, out, q_offsets, lse, batch: int, d: int, dtype, dev: int):
+        """(tokens, q_heads, address of q_offsets, of lse, the rows' strides)."""
+        self._on_device(dev)
+        if q.dim() != 3:
+            raise SttmError(STTM_ERR_SHAPE, "q must be [tokens, q_heads, head_dim]")
+        tokens, heads = q.shape[0], q.shape[1]
+        return (tokens, heads, _vector(q_offsets, "q_offsets", torch.int64, batch + 1, dev), _vector(lse, "lse", torch.float32, tokens * heads, dev),
+                _rows(q, "q", tokens, heads, d, dtype, dev), _rows(out, "out", tokens, heads, d, dtype, dev))
+
+    def sttm_cross_attention(self, q, states: States, out, scale: float, q_offsets=None, key_bias=None, lse=None, workspace=None):
+        """q, out [tokens, q_heads, d]; q_offsets int64 [batch + 1] (None: one token a sequence); key_bias float32 [rows] or [kv_heads, rows];
+        lse float32 [tokens, q_heads]; workspace: sttm_cross_attention_workspace_bytes() bytes."""
+        dev = states.device
+        tokens, heads, offsets, lse_at, qs, os_ = self._queries(q, out, q_offsets, lse, states.batch, states.head_dim, states.dtype, dev)
+        bias_at, bias_stride = None, 0
+        if key_bias is not None:
+            if key_bias.dtype is not torch.float32 or key_bias.get_device() != dev:
+                raise SttmError(STTM_ERR_DTYPE, "key_bias must be float32 on the states' device")
+            if key_bias.shape not in ((states.rows,), (states.kv_heads, states.rows)) or (states.rows > 1 and key_bias.stride(-1) != 1):
+                raise SttmError(STTM_ERR_SHAPE, "key_bias must be [rows] or [kv_heads, rows], the rows contiguous")
+            bias_at = key_bias.data_ptr()
+            if key_bias.dim() == 2 and states.kv_heads > 1:
+                bias_stride = key_bias.stride(0)
+        ws, size = self._scratch(workspace, dev)
+        rc = _lib.sttm_cross_attention(self._h, states.ref, tokens, heads, scale, q.data_ptr(), qs, offsets, bias_at, bias_stride, out.data_ptr(), os_,
+                                       lse_at, ws, size)
+        if rc != STTM_OK:
+            self._check(rc)
+
+    def sttm_shared_attention(self, q, cache: PagedCache, prefixes: Optional[Sequences], group_offsets, sequences: Sequences, out, scale: float,
+                              q_offsets=None, prefix_bias=None, key_bias=None, lse=None, workspace=None):
+        """q, out [tokens, q_heads, d]; prefixes: of the groups (None, with group_offsets None: no prefix); group_offsets int32 [groups + 1];
+        q_offsets int64 [batch + 1] (None: one token a sequence); prefix_bias float32 [groups, kv_heads, slots], key_bias float32 [batch, kv_heads,
+        slots]; lse float32 [tokens, q_heads]; workspace: sttm_shared_attention_workspace_bytes() bytes."""
+        dev = cache.device
+        tokens, heads, offsets, lse_at, qs, os_ = self._queries(q, out, q_offsets, lse, sequences.batch, cache.head_dim, cache.dtype, dev)
+        if sequences.device != dev or (prefixes is not None and prefixes.device != dev):
+            raise SttmError(STTM_ERR_ARG, "sequences and prefixes must be on the cache's device")
+        groups_at, bias_at, slots, own_at, own_slots = None, None, 0, None, 0
+        if prefixes is not None:
+            if group_offsets is None:
+                raise SttmError(STTM_ERR_ARG, "prefixes without group_offsets")
+            groups_at = _vector(group_offsets, "group_offsets", torch.int32, prefixes.batch + 1, dev)
+            if prefix_bias is not None:
+                slots = prefix_bias.shape[-1]
+                bias_at = _table(prefix_bias, "prefix_bias", torch.float32, (prefixes.batch, cache.kv_heads, slots), dev)
+        elif prefix_bias is not None or group_offsets is not None:
+            raise SttmError(STTM_ERR_ARG, "prefix_bias or group_offsets without prefixes")
+        if key_bias is not None:
+            own_slots = key_bias.shape[-1]
+            own_at = _table(key_bias, "key_bias", torch.float32, (sequences.batch, cache.kv_heads, own_slots), dev)
+        ws, size = self._scratch(workspace, dev)
+        rc = _lib.sttm_shared_attention(self._h, cache.ref, prefixes.ref if prefixes is not None else None, groups_at, sequences.ref, tokens, heads,
+                                        scale, q.data_ptr(), qs, offsets, bias_at, slots, own_at, own_slots, out.data_ptr(), os_, lse_at, ws, size)
         if rc != STTM_OK:
             self._check(rc)
 

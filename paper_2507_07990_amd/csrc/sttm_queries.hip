@@ -1,0 +1,314 @@
+// Entry points of the attention of several queries: over the packed rows of a batch, and over a prefix that sequences of a paged cache share.
+#include "sttm_queries.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace sttm {
+namespace {
+
+constexpr int kJoinThreads = 256;
+
+// The sequence, and for a launch over groups its segment, that a token belongs to; -1: none.
+__device__ inline int sequence_of(const QueryArgs& a, long long token) {
+  if (a.batch == 0) return -1;
+  const int b = last_not_above(a.batch, token, [&](int i) { return first_token(a, i); });
+  return first_token(a, b) <= token && token < first_token(a, b + 1) ? b : -1;
+}
+__device__ inline int segment_of(const QueryArgs& a, int b) {
+  if (!a.cuts) return b;
+  if (a.segments == 0) return -1;
+  const int s = last_not_above(a.segments, b, [&](int i) { return clamped(a.cuts[i], a.batch); });
+  return clamped(a.cuts[s], a.batch) <= b && b < clamped(a.cuts[s + 1], a.batch) ? s : -1;
+}
+__device__ inline int parts_of(const QueryArgs& a, const KeyArgs& k, int b) {
+  const int s = segment_of(a, b);
+  if (s < 0) return 0;
+  long long first;
+  const int length = segment_length(k, s, &first);
+  return max((length + k.chunk - 1) / k.chunk, 1);
+}
+
+// A row's parts on a common maximum: those of the first launch, then those of the second. Four channels a thread, the parts dealt out
+// among as many groups of threads as there are, added up in a fixed order. Tokens of no sequence stay as they are.
+template <int DT>
+__global__ void __launch_bounds__(kJoinThreads) k_query_join(QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb) {
+  __shared__ float4 sums[kJoinThreads];
+  constexpr int ES = DT == 0 ? 4 : 2;
+  const long long token = blockIdx.x;
+  const int head = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int seq = sequence_of(b, token);
+  if (seq < 0) return;
+  const int of_a = ka.chunks ? parts_of(a, ka, seq) : 0, of_b = parts_of(b, kb, seq), n = of_a + of_b;
+  const long long index = token * (b.kv_heads * b.group) + head;
+  const float2* stat = b.stat + index * b.parts;
+  auto at = [&](int i) { return i < of_a ? i : b.first_part + i - of_a; };
+  float top = -INFINITY, total = 0.f;
+  for (int i = lane; i < n; i += kWave) top = fmaxf(top, stat[at(i)].x);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  for (int i = lane; i < n; i += kWave) total = fmaf(stat[at(i)].y, query_factor(stat[at(i)].x, top), total);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+  if (tid == 0 && b.lse) b.lse[index] = top + logf(total);
+  const int units = b.d / 4, slices = kJoinThreads / units, unit = tid % units, slice = tid / units;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (slice < slices) {
+    for (int i = slice; i < n; i += slices) {
+      const float4 y = *reinterpret_cast<const float4*>(b.part + (index * b.parts + at(i)) * b.d + 4 * unit);
+      const float f = query_factor(stat[at(i)].x, top);
+      x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+    }
+  }
+  sums[tid] = x;
+  __syncthreads();
+  if (slice != 0) return;
+  for (int i = 1; i < slices; ++i) {
+    const float4 y = sums[i * units + unit];
+    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+  }
+  const float f = total == 0.f ? 0.f : 1.f / total;
+  char* out = b.out + token * b.out_stride + ((long long)head * b.d + 4 * unit) * ES;
+  if constexpr (DT == 0) *reinterpret_cast<float4*>(out) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+  else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<DT>(x.x * f, x.y * f), pack2<DT>(x.z * f, x.w * f));
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------
+
+// How the keys of one kind of segment are cut.
+struct Cut {
+  bool few;
+  int chunk, chunks;
+};
+Cut make_cut(int64_t tokens, int group, int segments, int kv_heads, int64_t max_len, int d, int es) {
+  Cut c{false, 64, 1};
+  if (segments < 1) return c;
+  const int64_t rows = tokens * group;
+  c.few = rows <= (int64_t)kRowTile * segments && query_row_bytes(d, es) <= 512;
+  const int64_t tiles = (rows / query_tile(c.few) + std::min<int64_t>(segments, rows)) * kv_heads;
+  const int least = c.few ? 256 : 512;
+  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / std::max<int64_t>(tiles, 1), (max_len + least - 1) / least, 512}));
+  const int64_t chunk = ((max_len + chunks - 1) / chunks + 127) / 128 * 128;
+  c.chunk = (int)std::max<int64_t>(chunk, 128);
+  c.chunks = (int)std::max<int64_t>(1, (max_len + c.chunk - 1) / c.chunk);
+  return c;
+}
+
+struct Plan {
+  Cut a, b;          // segments of several sequences (none: no chunks), segments of one
+  int parts;
+  size_t part, stat, bytes;
+};
+Plan make_plan(Cut a, Cut b, int64_t tokens, int q_heads, int d) {
+  Plan p{a, b, a.chunks + b.chunks, 0, 0, 0};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
+  const size_t rows = p.parts > 1 ? (size_t)tokens * q_heads * p.parts : 0;
+  p.part = take(rows * d * sizeof(float));
+  p.stat = take(rows * sizeof(float2));
+  p.bytes = std::max(off, (size_t)256);
+  return p;
+}
+
+int check_queries(sttm_ctx* ctx, int64_t tokens, int batch, int q_heads, int kv_heads, int64_t max_len) {
+  if (tokens < 0 || tokens > (1ll << 22)) return ctx_fail(ctx, STTM_ERR_SHAPE, "need 0 <= tokens <= 2^22");
+  if (q_heads < 1 || q_heads % kv_heads || q_heads / kv_heads > 256 || q_heads > 65535)
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "need q_heads a multiple of kv_heads, at most 256 a kv head, q_heads <= 65535");
+  if (tokens * (q_heads / kv_heads) > (1ll << 28)) return ctx_fail(ctx, STTM_ERR_SHAPE, "need tokens * q_heads / kv_heads <= 2^28");
+  if ((double)tokens * q_heads * max_len > 1e15) return ctx_fail(ctx, STTM_ERR_SHAPE, "tokens * q_heads * keys too large");
+  (void)batch;
+  return STTM_OK;
+}
+
+int check_states(sttm_ctx* c, const sttm_states* s) {
+  if (!s) return ctx_fail(c, STTM_ERR_NULL, "states is NULL");
+  if (s->dtype != STTM_F32 && s->dtype != STTM_BF16 && s->dtype != STTM_F16)
+    return ctx_fail(c, STTM_ERR_DTYPE, "dtype must be STTM_F32, STTM_BF16 or STTM_F16");
+  if (s->head_dim < 8 || s->head_dim > 256 || s->head_dim % 8 || s->kv_heads < 1 || s->kv_heads > 1024 || s->rows < 0 || s->rows > (1ll << 40) ||
+      s->batch < 0 || s->batch > 65535 || s->max_rows < 0 || s->max_rows > 1 << 30)
+    return ctx_fail(c, STTM_ERR_SHAPE, "need head_dim % 8 == 0, 8 <= head_dim <= 256, 1 <= kv_heads <= 1024, 0 <= rows <= 2^40, 0 <= batch <= 65535, 0 <= max_rows <= 2^30");
+  const int64_t align = 16 / elem_bytes(s->dtype), most = (int64_t)1 << 40;
+  if (s->row_stride < 0 || s->head_stride < 0 || s->row_stride > most || s->head_stride > most || s->row_stride % align || s->head_stride % align ||
+      (double)s->row_stride * (double)s->rows > 4e18 / elem_bytes(s->dtype))
+    return ctx_fail(c, STTM_ERR_SHAPE, "strides of the states: multiples of 16 bytes, not negative, within the address space");
+  if (s->batch && !s->offsets) return ctx_fail(c, STTM_ERR_NULL, "offsets is NULL");
+  if (s->batch && s->rows && s->max_rows && (!s->k || !s->v)) return ctx_fail(c, STTM_ERR_NULL, "k or v of the states is NULL");
+  if (!aligned16(s->k) || !aligned16(s->v)) return ctx_fail(c, STTM_ERR_ARG, "k and v must be 16-byte aligned");
+  return STTM_OK;
+}
+
+// What both calls ask of queries, results and scale, in the order in which they are looked at.
+int check_rows(sttm_ctx* ctx, int dtype, int head_dim, int q_heads, int64_t tokens, int batch, const void* q, int64_t q_stride, const void* out,
+               int64_t out_stride, const int64_t* q_offsets, float scale) {
+  const int64_t align = 16 / elem_bytes(dtype), row = (int64_t)q_heads * head_dim, most = (int64_t)1 << 40;
+  if (q_stride < row || out_stride < row || q_stride > most || out_stride > most || q_stride % align || out_stride % align)
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "q_stride, out_stride: multiples of 16 bytes, no less than a row");
+  if (!q_offsets && tokens != batch) return ctx_fail(ctx, STTM_ERR_SHAPE, "without q_offsets there is one token for each sequence");
+  if (!(std::fabs(scale) <= 3e38f)) return ctx_fail(ctx, STTM_ERR_ARG, "scale must be a finite number");
+  if (tokens && batch && (!q || !out)) return ctx_fail(ctx, STTM_ERR_NULL, "q or out is NULL");
+  if (!aligned16(q) || !aligned16(out)) return ctx_fail(ctx, STTM_ERR_ARG, "q and out must be 16-byte aligned");
+  return STTM_OK;
+}
+
+// Scales that the softmax can take into its exponent: no product of a difference of scores with one leaves fp32's range at either end.
+bool ordinary(float scale) { return scale >= 1e-30f && scale <= 1e30f; }
+
+Plan plan_cross(const sttm_states* s, int64_t tokens, int q_heads) {
+  const Cut b = make_cut(tokens, q_heads / s->kv_heads, s->batch, s->kv_heads, std::min<int64_t>(s->max_rows, s->rows), s->head_dim, elem_bytes(s->dtype));
+  return make_plan(Cut{false, 1, 0}, b, tokens, q_heads, s->head_dim);
+}
+
+Plan plan_shared(const sttm_cache* c, const sttm_sequences* prefixes, const sttm_sequences* seqs, int64_t tokens, int q_heads) {
+  const int group = q_heads / c->kv_heads, es = elem_bytes(c->dtype);
+  Cut a{false, 1, 0};
+  if (prefixes && prefixes->batch) a = make_cut(tokens, group, prefixes->batch, c->kv_heads, make_seqs(c, prefixes).max_len, c->head_dim, es);
+  return make_plan(a, make_cut(tokens, group, seqs->batch, c->kv_heads, make_seqs(c, seqs).max_len, c->head_dim, es), tokens, q_heads, c->head_dim);
+}
+
+template <int DT> void launch_all(QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb, const Plan& p, hipStream_t s) {
+  if (p.a.chunks) launch_queries<DT>(a, ka, p.a.few, s);
+  launch_queries<DT>(b, kb, p.b.few, s);
+  if (p.parts > 1) hipLaunchKernelGGL((k_query_join<DT>), dim3((unsigned)b.tokens, b.kv_heads * b.group), dim3(kJoinThreads), 0, s, a, ka, b, kb);
+}
+
+int launch(sttm_ctx* ctx, int dtype, QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb, const Plan& p, char* ws) {
+  const int rc = ctx_device(ctx);
+  if (rc != STTM_OK) return rc;
+  if (p.parts > 1) {
+    a.part = b.part = reinterpret_cast<float*>(ws + p.part);
+    a.stat = b.stat = reinterpret_cast<float2*>(ws + p.stat);
+  }
+  a.parts = b.parts = p.parts;
+  a.first_part = 0;
+  b.first_part = p.a.chunks;
+  ka.chunk = p.a.chunk; ka.chunks = p.a.chunks;
+  kb.chunk = p.b.chunk; kb.chunks = p.b.chunks;
+  const hipStream_t s = ctx_stream(ctx);
+  if (dtype == STTM_F32) launch_all<0>(a, ka, b, kb, p, s);
+  else if (dtype == STTM_BF16) launch_all<1>(a, ka, b, kb, p, s);
+  else launch_all<2>(a, ka, b, kb, p, s);
+  return ctx_after_launch(ctx);
+}
+
+QueryArgs make_queries(int dtype, int64_t tokens, int batch, int q_heads, int kv_heads, int head_dim, float scale, const void* q, int64_t q_stride,
+                       const int64_t* q_offsets, void* out, int64_t out_stride, float* lse) {
+  QueryArgs a{};
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.q_stride = q_stride * elem_bytes(dtype);
+  a.out_stride = out_stride * elem_bytes(dtype);
+  a.offsets = reinterpret_cast<const long long*>(q_offsets);
+  a.tokens = tokens;
+  a.batch = a.segments = batch;
+  a.kv_heads = kv_heads;
+  a.group = q_heads / kv_heads;
+  a.d = head_dim;
+  a.scale = scale;
+  return a;
+}
+
+KeyArgs make_paged(const sttm_cache* c, const sttm_sequences* s, const float* bias, int64_t slots, float scale) {
+  KeyArgs k{};
+  const Seqs seqs = make_seqs(c, s);
+  k.pool = make_pool(c);
+  k.table = seqs.table;
+  k.lengths = seqs.lengths;
+  k.table_stride = seqs.table_stride;
+  k.max_len = seqs.max_len;
+  k.token_stride = k.pool.token_stride;
+  k.bias = bias;
+  k.bias_segment = c->kv_heads * slots;
+  k.bias_head = slots;
+  k.scaled = bias || !ordinary(scale);
+  return k;
+}
+
+}  // namespace
+}  // namespace sttm
+
+using namespace sttm;
+
+extern "C" size_t sttm_cross_attention_workspace_bytes(const sttm_states* states, int64_t tokens, int q_heads) {
+  if (check_states(nullptr, states) != STTM_OK) return 0;
+  if (check_queries(nullptr, tokens, states->batch, q_heads, states->kv_heads, std::min<int64_t>(states->max_rows, states->rows)) != STTM_OK) return 0;
+  return plan_cross(states, tokens, q_heads).bytes;
+}
+
+extern "C" int sttm_cross_attention(sttm_ctx* ctx, const sttm_states* states, int64_t tokens, int q_heads, float scale, const void* q,
+                                    int64_t q_stride, const int64_t* q_offsets, const float* key_bias, int64_t bias_stride, void* out,
+                                    int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return STTM_ERR_NULL;
+  int rc = check_states(ctx, states);
+  if (rc != STTM_OK) return rc;
+  const int64_t max_len = std::min<int64_t>(states->max_rows, states->rows);
+  rc = check_queries(ctx, tokens, states->batch, q_heads, states->kv_heads, max_len);
+  if (rc == STTM_OK) rc = check_rows(ctx, states->dtype, states->head_dim, q_heads, tokens, states->batch, q, q_stride, out, out_stride, q_offsets, scale);
+  if (rc != STTM_OK) return rc;
+  if (key_bias && bias_stride != 0 && (bias_stride < states->rows || bias_stride > (1ll << 40)))
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "bias_stride: zero, or no less than rows");
+  if (tokens == 0 || states->batch == 0) return STTM_OK;
+  const Plan p = plan_cross(states, tokens, q_heads);
+  rc = check_workspace(ctx, workspace, workspace_bytes, p.bytes);
+  if (rc != STTM_OK) return rc;
+  const QueryArgs b = make_queries(states->dtype, tokens, states->batch, q_heads, states->kv_heads, states->head_dim, scale, q, q_stride, q_offsets, out,
+                                   out_stride, lse);
+  const int64_t es = elem_bytes(states->dtype);
+  KeyArgs k{};
+  k.pool.k = static_cast<char*>(const_cast<void*>(states->k));
+  k.pool.v = static_cast<char*>(const_cast<void*>(states->v));
+  k.pool.head_stride = states->head_stride * es;
+  k.pool.row = (int)(states->head_dim * es);
+  k.offsets = reinterpret_cast<const long long*>(states->offsets);
+  k.rows = states->rows;
+  k.max_len = (int)max_len;
+  k.token_stride = states->row_stride * es;
+  k.bias = key_bias;
+  k.bias_head = bias_stride;
+  k.scaled = key_bias || !ordinary(scale);
+  return launch(ctx, states->dtype, QueryArgs{}, KeyArgs{}, b, k, p, static_cast<char*>(workspace));
+}
+
+extern "C" size_t sttm_shared_attention_workspace_bytes(const sttm_cache* cache, const sttm_sequences* prefixes, const sttm_sequences* seqs,
+                                                        int64_t tokens, int q_heads) {
+  if (check_cache(nullptr, cache) != STTM_OK || (prefixes && check_sequences(nullptr, cache, prefixes) != STTM_OK) ||
+      check_sequences(nullptr, cache, seqs) != STTM_OK)
+    return 0;
+  const int64_t max_len = (int64_t)make_seqs(cache, seqs).max_len + (prefixes ? make_seqs(cache, prefixes).max_len : 0);
+  if (check_queries(nullptr, tokens, seqs->batch, q_heads, cache->kv_heads, max_len) != STTM_OK) return 0;
+  return plan_shared(cache, prefixes, seqs, tokens, q_heads).bytes;
+}
+
+extern "C" int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_sequences* prefixes, const int32_t* group_offsets,
+                                     const sttm_sequences* seqs, int64_t tokens, int q_heads, float scale, const void* q, int64_t q_stride,
+                                     const int64_t* q_offsets, const float* prefix_bias, int64_t prefix_slots, const float* key_bias,
+                                     int64_t key_slots, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return STTM_ERR_NULL;
+  int rc = check_cache(ctx, cache);
+  if (rc == STTM_OK && prefixes) rc = check_sequences(ctx, cache, prefixes);
+  if (rc == STTM_OK) rc = check_sequences(ctx, cache, seqs);
+  if (rc != STTM_OK) return rc;
+  const int64_t prefix_len = prefixes ? make_seqs(cache, prefixes).max_len : 0, own_len = make_seqs(cache, seqs).max_len, most = (int64_t)1 << 40;
+  rc = check_queries(ctx, tokens, seqs->batch, q_heads, cache->kv_heads, prefix_len + own_len);
+  if (rc == STTM_OK) rc = check_rows(ctx, cache->dtype, cache->head_dim, q_heads, tokens, seqs->batch, q, q_stride, out, out_stride, q_offsets, scale);
+  if (rc != STTM_OK) return rc;
+  if ((prefix_bias && (prefix_slots < prefix_len || prefix_slots > most)) || (key_bias && (key_slots < own_len || key_slots > most)))
+    return ctx_fail(ctx, STTM_ERR_SHAPE, "a bias needs no fewer slots than the max_len of its sequences");
+  if (prefix_bias && !prefixes) return ctx_fail(ctx, STTM_ERR_ARG, "prefix_bias without prefixes");
+  if (prefixes && prefixes->batch && !group_offsets) return ctx_fail(ctx, STTM_ERR_NULL, "group_offsets is NULL");
+  if (tokens == 0 || seqs->batch == 0) return STTM_OK;
+  const Plan p = plan_shared(cache, prefixes, seqs, tokens, q_heads);
+  rc = check_workspace(ctx, workspace, workspace_bytes, p.bytes);
+  if (rc != STTM_OK) return rc;
+  const QueryArgs b = make_queries(cache->dtype, tokens, seqs->batch, q_heads, cache->kv_heads, cache->head_dim, scale, q, q_stride, q_offsets, out,
+                                   out_stride, lse);
+  KeyArgs kb = make_paged(cache, seqs, key_bias, key_slots, scale), ka{};
+  kb.causal = 1;
+  QueryArgs a = b;
+  if (p.a.chunks) {
+    a.cuts = group_offsets;
+    a.segments = prefixes->batch;
+    ka = make_paged(cache, prefixes, prefix_bias, prefix_slots, scale);
+  }
+  return launch(ctx, cache->dtype, a, ka, b, kb, p, static_cast<char*>(workspace));
+}
