@@ -402,6 +402,25 @@ int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, const sttm_seq
 size_t sttm_shared_attention_workspace_bytes(const sttm_cache* cache, const sttm_sequences* prefixes, const sttm_sequences* seqs,
                                              int64_t tokens, int q_heads);
 
+/* What follows a block of a layer, in one pass over n rows: y is the block's result, x what it is added to.
+ *   r = scale * x + gate * post(y),   h = pre(r)   (of the r that is not rounded yet)
+ * post, pre (NULL: rows stay): STTM_NORM_RMS z * weight / sqrt(mean(z^2) + eps) + bias, STTM_NORM_LAYER the same of z - mean(z); weight and
+ * bias of the rows' type, [width], either may be NULL. gate of the rows' type (NULL: 1): one number (gate_width 1, gate_stride 0), one a
+ * row (gate_width 1, gate_stride elements apart), one a channel (gate_width = width, gate_stride 0) or a row of its own for each row;
+ * gate_tanh: its hyperbolic tangent counts. y NULL: r = scale * x. Either of r and h may be NULL; each may be x or y with its stride
+ * (not both the same one; other overlaps are not allowed). Computed in fp32 (squares included: they have to stay in its range), rounded once. width % 8 == 0, 8 <= width <=
+ * 16384; n <= 2^25; rows and weights 16-byte aligned. Asynchronous. */
+typedef enum { STTM_NORM_RMS = 0, STTM_NORM_LAYER = 1 } sttm_norm_kind;
+typedef struct {
+  int kind; /* sttm_norm_kind */
+  float eps;
+  const void* weight; /* device */
+  const void* bias;   /* device */
+} sttm_norm;
+int sttm_residual_norm(sttm_ctx* ctx, int dtype, int64_t n, int width, const void* x_dev, int64_t x_stride, const void* y_dev,
+                       int64_t y_stride, const sttm_norm* post, const void* gate_dev, int64_t gate_stride, int gate_width, int gate_tanh,
+                       float scale, void* r_dev, int64_t r_stride, const sttm_norm* pre, void* h_dev, int64_t h_stride);
+
 /* ---- inspection ---------------------------------------------------------------------------------------- */
 
 /* Copies an internal table (device to device, asynchronous) into dst_dev; bytes must equal the table's size. */

@@ -32,10 +32,11 @@ EXPORTS = [
     "sttm_set_cell_dots", "sttm_invalidate", "sttm_reduce_noalloc", "sttm_reduce_noalloc_max_bytes",
     "sttm_reduce_noalloc_bytes", "sttm_qk_norm_rope", "sttm_paged_attention", "sttm_paged_attention_workspace_bytes",
     "sttm_cache_evict", "sttm_cache_evict_workspace_bytes", "sttm_cross_attention", "sttm_cross_attention_workspace_bytes",
-    "sttm_shared_attention", "sttm_shared_attention_workspace_bytes",
+    "sttm_shared_attention", "sttm_shared_attention_workspace_bytes", "sttm_residual_norm",
 ]
 STTM_MATCH_FIRST_PASSING, STTM_MATCH_TOPLEFT_ONLY, STTM_MATCH_MOST_SIMILAR = 0, 1, 2
 STTM_ORDER_RASTER, STTM_ORDER_ZSCAN = 0, 1
+STTM_NORM_RMS, STTM_NORM_LAYER = 0, 1
 STTM_KERNEL_PYRAMID_STATS, STTM_KERNEL_TEMPORAL_DOTS, STTM_KERNEL_REDUCE_GATHER = 0, 1, 2
 
 
@@ -63,6 +64,11 @@ class _StatesStruct(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
                 ("rows", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("offsets", C.c_void_p),
                 ("batch", C.c_int), ("max_rows", C.c_int)]
+
+
+class _NormStruct(C.Structure):
+    """sttm_norm"""
+    _fields_ = [("kind", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -118,6 +124,8 @@ def _declare(lib: C.CDLL) -> C.CDLL:
     lib.sttm_shared_attention.argtypes = [vp, cache, seqs, vp, seqs, i64, i, f, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz]
     lib.sttm_shared_attention_workspace_bytes.argtypes = [cache, seqs, seqs, i64, i]
     lib.sttm_shared_attention_workspace_bytes.restype = sz
+    norm = C.POINTER(_NormStruct)
+    lib.sttm_residual_norm.argtypes = [vp, i, i64, i, vp, i64, vp, i64, norm, vp, i64, i, i, f, vp, i64, norm, vp, i64]
     return lib
 
 
@@ -239,6 +247,25 @@ class States:
         self.struct = _StatesStruct(_ptr(k), _ptr(v), _DTYPES[k.dtype], self.kv_heads, self.head_dim, self.rows, strides[0], strides[1],
                                     _ptr(offsets), self.batch, min(self.max_rows, 2**31 - 1))
         self.ref = C.byref(self.struct)
+
+
+class Norm:
+    """sttm_norm: STTM_NORM_RMS or STTM_NORM_LAYER; weight, bias [width] or None."""
+
+    def __init__(self, kind: int, weight=None, bias=None, eps: float = 1e-6):
+        for t, name in ((weight, "weight"), (bias, "bias")):
+            _expect(t is None or (t.dim() == 1 and t.is_contiguous()), STTM_ERR_SHAPE, f"the {name} of a norm must be [width], contiguous")
+            _expect(t is None or t.dtype in _DTYPES, STTM_ERR_DTYPE, f"the {name} of a norm must be float32, bfloat16 or float16")
+        self.weight, self.bias = weight, bias
+        self.struct = _NormStruct(kind, eps, _ptr(weight), _ptr(bias))
+        self.ref = C.byref(self.struct)
+
+    def _check_for(self, dtype, width: int, device: int):
+        for t in (self.weight, self.bias):
+            if t is not None and (t.dtype is not dtype or t.get_device() != device or t.numel() != width):
+                raise SttmError(STTM_ERR_SHAPE if t.dtype is dtype and t.get_device() == device else STTM_ERR_DTYPE,
+                                f"weight and bias of a norm must be {width} numbers of the rows' type on their device")
+        return self.ref
 
 
 def sttm_cross_attention_workspace_bytes(states: States, tokens: int, q_heads: int) -> int:
@@ -547,6 +574,38 @@ class Sttm:
         ws, size = self._scratch(workspace, dev)
         rc = _lib.sttm_shared_attention(self._h, cache.ref, prefixes.ref if prefixes is not None else None, groups_at, sequences.ref, tokens, heads,
                                         scale, q.data_ptr(), qs, offsets, bias_at, slots, own_at, own_slots, out.data_ptr(), os_, lse_at, ws, size)
+        if rc != STTM_OK:
+            self._check(rc)
+
+    def sttm_residual_norm(self, x, y, r, h, post: Optional[Norm] = None, pre: Optional[Norm] = None, gate=None, gate_tanh: bool = False,
+                           scale: float = 1.0):
+        """x, y, r, h [n, width] (y, r, h: None where there is none); gate [1 or n, 1 or width]: r = scale * x + gate * post(y), h = pre(r)."""
+        if x.dim() != 2:
+            raise SttmError(STTM_ERR_SHAPE, "x must be [n, width]")
+        (n, width), dtype, dev = x.shape, x.dtype, x.get_device()
+        self._on_device(dev)
+        if dtype not in _DTYPES:
+            raise SttmError(STTM_ERR_DTYPE, "float32, bfloat16 or float16")
+        rows = []
+        for t, name in ((x, "x"), (y, "y"), (r, "r"), (h, "h")):
+            if t is None:
+                rows += [None, width]
+                continue
+            if t.dtype is not dtype or t.get_device() != dev:
+                raise SttmError(STTM_ERR_DTYPE, f"{name} must be of the type and on the device of x")
+            if t.shape != (n, width) or (width > 1 and t.stride(1) != 1):
+                raise SttmError(STTM_ERR_SHAPE, f"{name} must be [{n}, {width}] with contiguous rows")
+            rows += [t.data_ptr(), t.stride(0) if n > 1 else width]
+        gate_at, gate_stride, gate_width = None, 0, 1
+        if gate is not None:
+            if gate.dtype is not dtype or gate.get_device() != dev:
+                raise SttmError(STTM_ERR_DTYPE, "gate must be of the type and on the device of x")
+            if gate.dim() != 2 or gate.shape[0] not in (1, n) or gate.shape[1] not in (1, width) or (gate.shape[1] > 1 and gate.stride(1) != 1):
+                raise SttmError(STTM_ERR_SHAPE, "gate must be [1 or n, 1 or width] with contiguous rows")
+            gate_at, gate_width, gate_stride = gate.data_ptr(), gate.shape[1], gate.stride(0) if gate.shape[0] > 1 else 0
+        rc = _lib.sttm_residual_norm(self._h, _DTYPES[dtype], n, width, *rows[:4], None if post is None else post._check_for(dtype, width, dev), gate_at,
+                                     gate_stride, gate_width, int(gate_tanh), scale, *rows[4:6], None if pre is None else pre._check_for(dtype, width, dev),
+                                     *rows[6:8])
         if rc != STTM_OK:
             self._check(rc)
 

@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsttm.so")
 SOURCES = ["sttm_api.hip", "sttm_spatial.hip", "sttm_temporal.hip", "sttm_reduce.hip", "sttm_rope.hip", "sttm_attention.hip",
-           "sttm_evict.hip", "sttm_queries.hip", "sttm_queries_f32.hip", "sttm_queries_bf16.hip", "sttm_queries_f16.hip"]
+           "sttm_evict.hip", "sttm_queries.hip", "sttm_queries_f32.hip", "sttm_queries_bf16.hip", "sttm_queries_f16.hip",
+           "sttm_residual.hip"]
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 VALU forms

@@ -16,7 +16,7 @@ SMALL = ["-DSTTM_CHUNK_MAX=32", "-DSTTM_ROPE_WAVES=1", "-DSTTM_ROPE_ONCE_BYTES=0
 LIB_SANITIZED = os.path.join(base.HERE, "libsttm_cache_cpu_sanitized.so")
 SANITIZE = ["-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer"]
 SOURCES = ["sttm_rope.hip", "sttm_attention.hip", "sttm_evict.hip", "sttm_queries.hip", "sttm_queries_f32.hip", "sttm_queries_bf16.hip",
-           "sttm_queries_f16.hip"]
+           "sttm_queries_f16.hip", "sttm_residual.hip"]
 
 
 def _flags():

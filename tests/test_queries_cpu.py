@@ -26,3 +26,4 @@ def bench():
 
 
 from tests.query_tests import *  # noqa: E402,F401,F403  -- the tests themselves, on this file's `bench`
+from tests.residual_tests import *  # noqa: E402,F401,F403

@@ -12,3 +12,4 @@ def bench(lib):
 
 
 from tests.query_tests import *  # noqa: E402,F401,F403  -- the tests that run on host threads too
+from tests.residual_tests import *  # noqa: E402,F401,F403
