@@ -366,7 +366,7 @@ size_t sttm_cache_evict_workspace_bytes(const sttm_cache* cache, const sttm_sequ
  * and of v and has head_dim elements (two parts of one projection's output will do). Sequence b has the rows offsets[b] ..
  * offsets[b + 1] - 1 (device int64 [batch + 1], ascending, e.g. the offsets of sttm_reduce), no more than max_rows of them (launches
  * are sized by it; rows behind it are not read, nor any behind `rows`). head_dim % 8 == 0, 8 <= head_dim <= 256; 1 <= kv_heads <= 1024; k, v and strides
- * multiples of 16 bytes; max_rows <= 2^30; batch <= 65535. */
+ * multiples of 16 bytes; row_stride <= 2^22; max_rows <= 2^30; batch <= 65535. */
 typedef struct {
   const void* k; /* device */
   const void* v; /* device */

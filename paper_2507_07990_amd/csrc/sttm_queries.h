@@ -89,7 +89,7 @@ __device__ inline float query_factor(float m, float top) { return exp2_fast((m -
 template <int DT> void launch_queries(const QueryArgs& a, const KeyArgs& k, bool few_rows, hipStream_t s);
 // Rows of a workgroup's tile for this kind.
 inline int query_tile(bool few_rows) { return few_rows ? kRowTile : kRowTile * kQueryWaves; }
-// Bytes of a head's row in LDS; above 512 a tile of its own for each wavefront would not fit.
-inline int query_row_bytes(int d, int es) { return es * (d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256); }
+// Bytes of a head's row in LDS: a power of two; above 512 a tile of its own for each wavefront would not fit.
+constexpr int query_row_bytes(int d, int es) { return d * es <= 128 ? 128 : d * es <= 256 ? 256 : d * es <= 512 ? 512 : 1024; }
 
 }  // namespace sttm

@@ -128,9 +128,8 @@ int check_states(sttm_ctx* c, const sttm_states* s) {
       s->batch < 0 || s->batch > 65535 || s->max_rows < 0 || s->max_rows > 1 << 30)
     return ctx_fail(c, STTM_ERR_SHAPE, "need head_dim % 8 == 0, 8 <= head_dim <= 256, 1 <= kv_heads <= 1024, 0 <= rows <= 2^40, 0 <= batch <= 65535, 0 <= max_rows <= 2^30");
   const int64_t align = 16 / elem_bytes(s->dtype), most = (int64_t)1 << 40;
-  if (s->row_stride < 0 || s->head_stride < 0 || s->row_stride > most || s->head_stride > most || s->row_stride % align || s->head_stride % align ||
-      (double)s->row_stride * (double)s->rows > 4e18 / elem_bytes(s->dtype))
-    return ctx_fail(c, STTM_ERR_SHAPE, "strides of the states: multiples of 16 bytes, not negative, within the address space");
+  if (s->row_stride < 0 || s->head_stride < 0 || s->row_stride > 1 << 22 || s->head_stride > most || s->row_stride % align || s->head_stride % align)
+    return ctx_fail(c, STTM_ERR_SHAPE, "strides of the states: multiples of 16 bytes, not negative, row_stride at most 2^22");
   if (s->batch && !s->offsets) return ctx_fail(c, STTM_ERR_NULL, "offsets is NULL");
   if (s->batch && s->rows && s->max_rows && (!s->k || !s->v)) return ctx_fail(c, STTM_ERR_NULL, "k or v of the states is NULL");
   if (!aligned16(s->k) || !aligned16(s->v)) return ctx_fail(c, STTM_ERR_ARG, "k and v must be 16-byte aligned");

@@ -101,18 +101,15 @@ inline void settle() {}
 inline void to_lds(const char* from, char* base) { memcpy(base + 16 * (threadIdx.x & 63), from, 16); }
 inline void arrived() {}
 #define __builtin_amdgcn_sched_barrier(x) ((void)0)
+#define __builtin_amdgcn_readlane(x, i) __shfl(x, i)
 #endif
 
-// Pieces of 16 bytes of a row of CH pieces are kept in an order of the row's own, so that the lanes that read a column of pieces
-// (keys: sixteen rows; values: four rows of 64 bytes) find them in different banks of LDS.
-template <int CH> __device__ inline int key_place(int row, int piece) {
-  constexpr int P = CH % 16 == 0 ? 16 : CH % 8 == 0 ? 8 : 4;
-  return row * CH + (piece ^ ((row / (16 / P)) & (P - 1)));
-}
-template <int DT, int CH> __device__ inline int value_place(int row, int piece) {
-  constexpr int P = CH % 16 == 0 ? 16 : CH % 8 == 0 ? 8 : 4;
-  if constexpr (DT == 0) return row * CH + (P == 16 ? piece ^ (8 * ((row >> 2) & 1)) : piece);
-  return row * CH + (piece ^ (4 * ((row / (16 / P)) & (P / 4 - 1))));
+// A row has CH pieces of 16 bytes in LDS (a power of two), in an order of its own, so that the lanes that read a column of pieces (keys:
+// sixteen rows; values: four rows of 64 bytes) find them in different banks.
+template <int CH> __device__ inline int key_order(int row) { return CH >= 16 ? row & 15 : (row >> 1) & 7; }
+template <int DT, int CH> __device__ inline int value_order(int row) {
+  if constexpr (DT == 0) return CH >= 16 ? 8 * ((row >> 2) & 1) : 0;
+  return CH >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
 }
 
 // Of a word with two 16-bit numbers (fp32: one), those that are neither infinite nor NaN.
@@ -124,15 +121,17 @@ template <int DT> __device__ inline uint32_t finite_only(uint32_t x) {
 
 // How a workgroup is made up: wavefronts (two buffers each have to fit LDS where a wavefront has blocks of its own), keys of a block, sixteen-byte
 // pieces that a thread brings of it.
-constexpr int query_waves(int dt, int dp, bool few) { return few && dp * (dt == 0 ? 4 : 2) > 256 ? 2 : kQueryWaves; }
-constexpr int query_blocks_a_unit(int dt, int dp, bool few) { return few || dp * (dt == 0 ? 4 : 2) > 256 ? 1 : 2; }
+constexpr int query_waves(int dt, int dp, bool few) { return few && query_row_bytes(dp, dt == 0 ? 4 : 2) > 256 ? 2 : kQueryWaves; }
+constexpr int query_blocks_a_unit(int dt, int dp, bool few) { return few || query_row_bytes(dp, dt == 0 ? 4 : 2) > 256 ? 1 : 2; }
 template <int DT, int DP, bool FEW> struct Shape {
-  static constexpr int ES = DT == 0 ? 4 : 2, ROW = DP * ES, CH = ROW / 16, NQ = CH / 2, M = DP / 32;
+  static constexpr int ES = DT == 0 ? 4 : 2, M = DP / 32, NQ = DP * ES / 32;
+  static constexpr int ROW = query_row_bytes(DP, ES), CH = ROW / 16;
   static constexpr int WAVES = query_waves(DT, DP, FEW), THREADS = WAVES * kWave;
   static constexpr int SHARE = FEW ? 1 : WAVES;           // wavefronts that share a block of keys
   static constexpr int SETS = WAVES / SHARE;
   static constexpr int NK = !FEW && ROW <= 256 ? 64 : 32, KT = NK / 32;
-  static constexpr int LOADERS = SHARE * kWave, PER = NK * CH / LOADERS;
+  static constexpr int AT_ONCE = kWave / CH;              // rows of one load of a wavefront
+  static constexpr int PER = NK / (AT_ONCE * SHARE);      // loads of a wavefront for a block's keys
   static constexpr int TILE = kRowTile * SHARE;
 };
 
@@ -151,10 +150,11 @@ template <int DT, int DP, bool FEW>
 __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks_a_unit(DT, DP, FEW)) k_query_tiles(QueryArgs a, KeyArgs kk) {
   using S = Shape<DT, DP, FEW>;
   constexpr int ES = S::ES, ROW = S::ROW, CH = S::CH, NQ = S::NQ, M = S::M, SETS = S::SETS, NK = S::NK, KT = S::KT;
-  constexpr int LOADERS = S::LOADERS, PER = S::PER, TILE = S::TILE, THREADS = S::THREADS;
+  constexpr int AT_ONCE = S::AT_ONCE, PER = S::PER, TILE = S::TILE, THREADS = S::THREADS;
   constexpr float LIFT = DT == 2 ? 15.f : 0.f;
   constexpr float UNLIFT = DT == 2 ? 1.f / 32768.f : 1.f;
-  static_assert(NK * CH % LOADERS == 0 && (!FEW || SETS * 2 * NK * ROW * 2 >= S::WAVES * 4096), "tiles");
+  constexpr bool WIDE = DP * ES > 256;                    // one way for all blocks: the registers that two ways take are not there
+  static_assert(CH >= 8 && CH <= 64 && NK % (AT_ONCE * S::SHARE) == 0 && (!FEW || SETS * 2 * NK * ROW * 2 >= S::WAVES * 4096), "tiles");
 
   __shared__ __align__(16) char tiles[SETS][2][2][NK * ROW];  // of each set two buffers of keys and of values
   __shared__ __align__(16) float adds[SETS][2][NK];       // what is added to a key's score: its bias; -inf: it does not count
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
   if (first >= length && chunk > 0) return;               // (an empty segment's first chunk is gone through: its result is written)
 
   // This lane's row.
-  const int set = FEW ? wave : 0, share = FEW ? 0 : wave, u = FEW ? lane : tid;
+  const int set = FEW ? wave : 0, share = FEW ? 0 : wave;
   const long long row = row0 + share * kRowTile + i32;
   const bool mine = row < rows;
   const long long in_row = min(row, rows - 1), in_token = in_row / a.group, token = token0 + in_token;
@@ -202,52 +202,72 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
 
   const float* bias = kk.bias ? kk.bias + s * kk.bias_segment + h * kk.bias_head + key0 : nullptr;
   const int32_t* table = kk.table ? kk.table + s * kk.table_stride : nullptr;
+  const int page_mask = (1 << kk.pool.shift) - 1;
   const long long base = h * kk.pool.head_stride + key0 * kk.token_stride;
-  const int page_mask = kk.table ? (1 << kk.pool.shift) - 1 : 0x7fffffff;
+  const int stride = (int)kk.token_stride;                // (a block's rows lie within 2 GiB)
 
-  // The pieces of LDS that this thread fills: of the block's rows, the pieces of channels that there are. The others stay zero.
-  int piece_row[PER], key_piece[PER], value_piece[PER], page_next[PER];
+  // The pieces of LDS that this lane fills with load i: of row brought + AT_ONCE * SHARE * i (+ its own row of the AT_ONCE of a load), which lie
+  // in one page. Pieces behind a head's channels stay zero.
+  const int brought = __builtin_amdgcn_readfirstlane(share * AT_ONCE), own_row = lane / CH;
+  int key_from[PER], value_from[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int p = u + i * LOADERS;
-    piece_row[i] = p / CH;
-    key_piece[i] = 16 * (key_place<CH>(p / CH, p % CH) % CH);
-    value_piece[i] = 16 * (value_place<DT, CH>(p / CH, p % CH) % CH);
+    const int r = brought + AT_ONCE * S::SHARE * i + own_row;
+    key_from[i] = 16 * (lane % CH ^ key_order<CH>(r));
+    value_from[i] = 16 * (lane % CH ^ value_order<DT, CH>(r));
   }
-  const int in_wave = 16 * kWave * (FEW ? 0 : wave);
-  // A block's slots: their pages are looked up a block ahead. Slots from the end on are read as the last one; one whose page is not in
-  // the pool is not read.
+  const bool full = kk.pool.row == ROW;
+  // Lane i: the page of the block's key i, looked up a block ahead, and what is added to its score. Keys from the end on: the page of the
+  // last one, whose other slots may be read.
+  int page_next = 0;
+  float add_next = 0.f;
   auto look_up = [&](int s0) {
-    if (!table) return;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) page_next[i] = table[min(s0 + piece_row[i], end - 1) >> kk.pool.shift];
+    if (table) page_next = table[min(s0 + min(lane, NK - 1), end - 1) >> kk.pool.shift];
   };
-  auto offset_of = [&](int slot, int page) -> long long {  // of a slot's row, -1: its page is not in the pool
-    if (!table) return base + slot * kk.token_stride;
-    return page >= 0 && page < kk.pool.pages ? page * kk.pool.page_stride + base + (slot & page_mask) * kk.token_stride : -1;
-  };
-  // Where this lane reads in LDS: the parts of an address that rows of a fixed distance have in common.
-  constexpr int P = CH % 16 == 0 ? 16 : CH % 8 == 0 ? 8 : 4, NK_AT = NQ < P / 2 ? NQ : P / 2, NV_AT = DT != 0 ? M : P == 16 ? 2 : 1;
-  int key_at[NK_AT], value_at[NV_AT];
-#pragma unroll
-  for (int i = 0; i < NK_AT; ++i) key_at[i] = 16 * key_place<CH>(i32, 2 * i + g);
-#pragma unroll
-  for (int i = 0; i < NV_AT; ++i) {
-    if constexpr (DT == 0) value_at[i] = 16 * value_place<DT, CH>(4 * g, 8 * i + i32 / 4) + 4 * (i32 % 4);
-    else value_at[i] = 16 * value_place<DT, CH>(4 * g + (lane & 15) / 4, 4 * i + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) + 8 * (lane & 1);
-  }
-  float add_next = 0.f;                                   // lane i: of key i
   auto load = [&](int s0, int buffer) {
-    const int slot = min(s0 + lane, end - 1);
-    add_next = bias ? bias[slot] : 0.f;
-    if (lane >= NK || s0 + lane >= end || (table && (unsigned)table[slot >> kk.pool.shift] >= (unsigned)kk.pool.pages)) add_next = -INFINITY;
+    const bool there = !table || (unsigned)page_next < (unsigned)kk.pool.pages;
+    add_next = bias ? bias[min(s0 + min(lane, NK - 1), end - 1)] : 0.f;
+    if (lane >= NK || s0 + lane >= end || !there) add_next = -INFINITY;
+    const int page = there ? page_next : 0;               // (what is read of a page that is not there does not count)
+    char* const to = tiles[set][buffer][0] + brought * ROW;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const long long at = offset_of(min(s0 + piece_row[i], end - 1), page_next[i]);
-      if (at >= 0 && key_piece[i] < kk.pool.row) to_lds(kk.pool.k + at + key_piece[i], tiles[set][buffer][0] + in_wave + 16 * i * LOADERS);
-      if (at >= 0 && value_piece[i] < kk.pool.row) to_lds(kk.pool.v + at + value_piece[i], tiles[set][buffer][1] + in_wave + 16 * i * LOADERS);
+      const int r = brought + AT_ONCE * S::SHARE * i;
+      long long from;
+      int row = own_row * stride;
+      if (table) {
+        from = __builtin_amdgcn_readlane(page, r) * kk.pool.page_stride + base + ((s0 + r) & page_mask) * stride;
+      } else {
+        from = base + (s0 + r) * kk.token_stride;
+        if (s0 + NK > end) {                              // (rows from the end on: the last one)
+          from = base + s0 * kk.token_stride;
+          row = min(r + own_row, end - 1 - s0) * stride;
+        }
+      }
+      char* const at = to + AT_ONCE * S::SHARE * i * ROW;
+      if (full) {
+        to_lds(kk.pool.k + from + (unsigned)(row + key_from[i]), at);
+        to_lds(kk.pool.v + from + (unsigned)(row + value_from[i]), at + NK * ROW);
+      } else {
+        if (key_from[i] < kk.pool.row) to_lds(kk.pool.k + from + (unsigned)(row + key_from[i]), at);
+        if (value_from[i] < kk.pool.row) to_lds(kk.pool.v + from + (unsigned)(row + value_from[i]), at + NK * ROW);
+      }
     }
   };
+
+  // Where this lane reads in LDS: the parts of an address that rows of a fixed distance have in common.
+  constexpr int P = CH >= 16 ? 16 : 8, NK_AT = NQ < P / 2 ? NQ : P / 2, NV_AT = DT != 0 ? M : M < 2 || CH < 16 ? 1 : 2;
+  int key_at[NK_AT], value_at[NV_AT];
+#pragma unroll
+  for (int i = 0; i < NK_AT; ++i) key_at[i] = i32 * ROW + 16 * ((2 * i + g) ^ key_order<CH>(i32));
+#pragma unroll
+  for (int i = 0; i < NV_AT; ++i) {
+    if constexpr (DT == 0) value_at[i] = 4 * g * ROW + 16 * ((8 * i + i32 / 4) ^ value_order<DT, CH>(4 * g)) + 4 * (i32 % 4);
+    else {
+      const int r = 4 * g + (lane & 15) / 4;
+      value_at[i] = r * ROW + 16 * ((4 * i + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) ^ value_order<DT, CH>(r)) + 8 * (lane & 1);
+    }
+  }
 
   f32x16 acc[M];
 #pragma unroll
@@ -255,10 +275,11 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[n][r] = 0.f;
   // Scores that have no bias stay as the product gives them, the scale is part of the exponent's factor.
-  float m = -INFINITY, l = 0.f;  // l: of this lane's keys
-  const float times = kk.scaled ? kLog2e : a.scale * kLog2e;
+  constexpr float kWide = 65536.f;                        // (times 2^-24 is what the rounding of `from` may leave in an exponent)
+  float m = -INFINITY, from = 0.f, l = 0.f;  // from: m as an exponent of two; l: of this lane's keys
+  const float times = kk.scaled ? kLog2e : a.scale * kLog2e, scaled = kk.scaled ? a.scale : 1.f;
   if (tid == 0) odd_value = 0;
-  if (16 * CH > kk.pool.row) {                            // pieces of LDS that nothing is loaded into
+  if (!full) {                                            // pieces of LDS that nothing is loaded into
     for (int i = tid; i < (int)sizeof(tiles) / 16; i += THREADS) reinterpret_cast<w4*>(tiles)[i] = w4{0u, 0u, 0u, 0u};
     __syncthreads();
   }
@@ -275,15 +296,17 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
     arrived();
     const unsigned long long alive = __ballot(add_next != -INFINITY);
     const bool whole = alive == (NK == 64 ? ~0ull : 0xffffffffull);
-    const bool diagonal = s0 + NK > least && least < length, careful = kk.scaled || diagonal || !whole;
+    const bool diagonal = s0 + NK > least && least < length, added = WIDE || kk.scaled || !whole;
     if (diagonal || !whole) {                             // (this wavefront's own pieces: it sees what it loaded)
       __builtin_amdgcn_wave_barrier();
       bool odd = false;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        w4* at = reinterpret_cast<w4*>(values + 16 * (u + i * LOADERS));
-        if (!(alive >> piece_row[i] & 1)) {
+        const int r = brought + AT_ONCE * S::SHARE * i;
+        w4* at = reinterpret_cast<w4*>(values + r * ROW + 16 * lane);
+        if (!(alive >> (r + own_row) & 1)) {              // a key that does not count: nothing of it may be infinite or NaN
           *at = w4{0u, 0u, 0u, 0u};
+          *reinterpret_cast<w4*>(keys + r * ROW + 16 * lane) = w4{0u, 0u, 0u, 0u};
         } else if (diagonal) {
           w4 y = *at;
 #pragma unroll
@@ -297,7 +320,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       }
       if (odd) odd_value = 1;
     }
-    if (share == 0 && lane < NK && careful) adds[set][buffer][lane] = add_next;
+    if (share == 0 && lane < NK && added) adds[set][buffer][lane] = add_next;
     if constexpr (FEW) __builtin_amdgcn_wave_barrier();
     else __syncthreads();
     if (s0 + step < end) {
@@ -312,7 +335,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       for (int r = 0; r < 16; ++r) x[t][r] = 0.f;
 #pragma unroll
     for (int c = 0; c < NQ; ++c) {
-      if (ROW > 256 && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // (not all reads before the first product: registers)
+      if (DP * ES > 256 && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // (not all reads before the first product: registers)
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
         const w4 k = *reinterpret_cast<const w4*>(keys + key_at[c % NK_AT] + (32 * t * ROW + c / NK_AT * NK_AT * 32));
@@ -325,7 +348,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       }
     }
     settle();
-    if (careful) {
+    if (added) {
 #pragma unroll
       for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -333,37 +356,47 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
           const float4 add = *reinterpret_cast<const float4*>(&adds[set][buffer][32 * t + 8 * r4 + 4 * g]);
           const float of[4] = {add.x, add.y, add.z, add.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float y = x[t][4 * r4 + e];
-            if (kk.scaled) y = fmaf(y, a.scale, of[e]);
-            if (of[e] == -INFINITY || s0 + 32 * t + 8 * r4 + 4 * g + e >= limit) y = -INFINITY;
-            x[t][4 * r4 + e] = y;
-          }
+          for (int e = 0; e < 4; ++e) x[t][4 * r4 + e] = fmaf(x[t][4 * r4 + e], scaled, of[e]);
         }
     }
-    float top = -INFINITY;
+    if (diagonal) {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (s0 + 32 * t + 8 * (r / 4) + 4 * g + r % 4 >= limit) x[t][r] = -INFINITY;
+    }
+    float top = x[0][0];
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[t][r]);
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     if (__ballot(top > m) != 0) {  // (seldom after the first blocks)
-      const float m2 = fmaxf(m, top), shrink = exp2_fast((m - (m2 == -INFINITY ? 0.f : m2)) * times);
-      m = m2;
+      const float before = m, from_before = m == -INFINITY ? -INFINITY : from;
+      m = fmaxf(m, top);
+      from = m == -INFINITY ? 0.f : m * times;
+      const float shrink = exp2_fast(fabsf(from) < kWide ? from_before - from : (before - m) * times);
       l *= shrink;
 #pragma unroll
       for (int n = 0; n < M; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[n][r] *= shrink;
     }
-    const float from = m == -INFINITY ? 0.f : m;
+    float less = LIFT - from;
+    if (WIDE || __ballot(!(fabsf(from) < kWide)) != 0) {  // large scores: no multiple of theirs, only of their differences
+      less = LIFT;
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[t][r] -= m == -INFINITY ? 0.f : m;
+    }
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = exp2_fast(DT == 2 ? fmaf(x[t][r] - from, times, LIFT) : (x[t][r] - from) * times);
-        x[t][r] = p;
-        l += p;
+        x[t][r] = exp2_fast(fmaf(x[t][r], times, less));
+        l += x[t][r];
       }
     if constexpr (DT == 0) {
 #pragma unroll
@@ -466,8 +499,9 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       float add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
       for (int i = max(first, least - NK + 1); i < min(end, limit); ++i) {
-        const long long at = offset_of(i, table ? table[i >> kk.pool.shift] : 0);
-        if (at < 0 || (bias && bias[i] == -INFINITY)) continue;
+        const int page = table ? table[i >> kk.pool.shift] : 0;
+        if ((table && (unsigned)page >= (unsigned)kk.pool.pages) || (bias && bias[i] == -INFINITY)) continue;
+        const long long at = base + (table ? page * kk.pool.page_stride + (i & page_mask) * stride : i * kk.token_stride);
         for (int e = 0; e < 4; ++e) {
           float v;
           if constexpr (DT == 0) v = *reinterpret_cast<const float*>(kk.pool.v + at + 4 * (c + e));

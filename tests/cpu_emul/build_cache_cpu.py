@@ -27,7 +27,7 @@ def build_sanitized() -> str:
     """(Its sources one by one, side by side: they take a minute or two.)"""
     if base._up_to_date(LIB_SANITIZED):
         return LIB_SANITIZED
-    flags = ["g++", "-std=c++17", "-O1", "-g1", "-pthread", "-I", base.HERE, "-I", base.CSRC, "-Wno-unknown-pragmas", "-Wno-attributes"]
+    flags = ["g++", "-std=c++17", "-O1", "-g1", "-pthread", "-I", base.HERE, "-I", base.CSRC, "-Wno-unknown-pragmas", "-Wno-psabi", "-Wno-attributes"]
     sources = [os.path.join(base.CSRC, s) for s in base.SOURCES + SOURCES] + [os.path.join(base.HERE, "emul.cpp")]
     with tempfile.TemporaryDirectory() as folder, ThreadPoolExecutor(4) as pool:
         def compiled(source):

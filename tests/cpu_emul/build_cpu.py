@@ -35,7 +35,7 @@ def _up_to_date(out):
 def _compile(flags, extra_sources, out, verbose):
     if _up_to_date(out):
         return out
-    cmd = ["g++", "-std=c++17", "-O1", "-g", "-pthread", "-I", HERE, "-I", CSRC, "-Wno-unknown-pragmas",
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-pthread", "-I", HERE, "-I", CSRC, "-Wno-unknown-pragmas", "-Wno-psabi",
            "-Wno-attributes"] + flags
     for s in [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(HERE, s) for s in ["emul.cpp"] + extra_sources]:
         cmd += ["-x", "c++", s]
