@@ -25,6 +25,7 @@ struct QueryArgs {
   float scale;
   float* part;                   // [tokens, q_heads, parts, d]: unnormalised sums (more than one part), else NULL
   float2* stat;                  // [tokens, q_heads, parts]: largest score and sum of exponentials of a part
+  int alone;                     // no other launch has parts of these rows: a segment of one chunk has its result right away
   int parts, first_part;         // parts of a row in all, and where this launch's chunks begin among them
 };
 
@@ -38,10 +39,10 @@ struct KeyArgs {
   long long rows;
   int max_len;
   long long token_stride;        // bytes
+  int from_each, slot_mask;      // pages: ~0, the slots of a page less one; packed: 0, all
   const float* bias;             // NULL: none. Of slot i: bias[segment * bias_segment + h * bias_head + i] (packed: + the first row)
   long long bias_segment, bias_head;
   int causal;                    // token j of a segment's n sees the slots before length - (n - 1 - j)
-  int scaled;                    // scores are formed before the softmax's maximum is taken (a bias, or a scale out of the ordinary)
   int chunk, chunks;
 };
 

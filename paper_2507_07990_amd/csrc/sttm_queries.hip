@@ -7,7 +7,7 @@
 namespace sttm {
 namespace {
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kJoinHeads = 4, kJoinWaves = 4096;  // (rows from which on a wavefront each)
 
 // The sequence, and for a launch over groups its segment, that a token belongs to; -1: none.
 __device__ inline int sequence_of(const QueryArgs& a, long long token) {
@@ -29,51 +29,65 @@ __device__ inline int parts_of(const QueryArgs& a, const KeyArgs& k, int b) {
   return max((length + k.chunk - 1) / k.chunk, 1);
 }
 
-// A row's parts on a common maximum: those of the first launch, then those of the second. Four channels a thread, the parts dealt out
-// among as many groups of threads as there are, added up in a fixed order. Tokens of no sequence stay as they are.
-template <int DT>
+// A row's parts on a common maximum: those of the first launch, then those of the second, added up in a fixed order. Tokens of no sequence stay
+// as they are, and rows whose only part is their result already.
+// LANES lanes have a row, four channels each, the parts dealt out among as many groups of lanes as there are. A workgroup where there are few rows (their
+// parts come from all over memory at once: 32 tokens, 28 heads, 58 parts of 128 channels 9 us), a wavefront with four of a token's heads in turn else.
+template <int DT, int LANES>
 __global__ void __launch_bounds__(kJoinThreads) k_query_join(QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb) {
   __shared__ float4 sums[kJoinThreads];
-  constexpr int ES = DT == 0 ? 4 : 2;
+  constexpr int ES = DT == 0 ? 4 : 2, HEADS = LANES == kJoinThreads ? 1 : kJoinHeads;
   const long long token = blockIdx.x;
-  const int head = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, u = tid & (LANES - 1);
   const int seq = sequence_of(b, token);
   if (seq < 0) return;
-  const int of_a = ka.chunks ? parts_of(a, ka, seq) : 0, of_b = parts_of(b, kb, seq), n = of_a + of_b;
-  const long long index = token * (b.kv_heads * b.group) + head;
-  const float2* stat = b.stat + index * b.parts;
+  const int of_a = ka.chunks ? parts_of(a, ka, seq) : 0, of_b = parts_of(b, kb, seq), n = of_a + of_b, heads = b.kv_heads * b.group;
+  if (b.alone && n == 1) return;
+  const int units = b.d / 4, slices = LANES / units, unit = u % units, slice = u / units;
   auto at = [&](int i) { return i < of_a ? i : b.first_part + i - of_a; };
-  float top = -INFINITY, total = 0.f;
-  for (int i = lane; i < n; i += kWave) top = fmaxf(top, stat[at(i)].x);
+  for (int i = 0; i < HEADS; ++i) {
+    const int head = (blockIdx.y * (kJoinThreads / LANES) + tid / LANES) * HEADS + i;
+    if (head >= heads) return;                            // (all lanes of a row)
+    const long long index = token * heads + head;
+    const float2* stat = b.stat + index * b.parts;
+    float top = -INFINITY, total = 0.f;
+    for (int p = lane; p < n; p += kWave) top = fmaxf(top, stat[at(p)].x);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  for (int i = lane; i < n; i += kWave) total = fmaf(stat[at(i)].y, query_factor(stat[at(i)].x, top), total);
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    for (int p = lane; p < n; p += kWave) total = fmaf(stat[at(p)].y, query_factor(stat[at(p)].x, top), total);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-  if (tid == 0 && b.lse) b.lse[index] = top + logf(total);
-  const int units = b.d / 4, slices = kJoinThreads / units, unit = tid % units, slice = tid / units;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (slice < slices) {
-    for (int i = slice; i < n; i += slices) {
-      const float4 y = *reinterpret_cast<const float4*>(b.part + (index * b.parts + at(i)) * b.d + 4 * unit);
-      const float f = query_factor(stat[at(i)].x, top);
-      x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    if (u == 0 && b.lse) b.lse[index] = top + logf(total);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (slice < slices) {
+#pragma unroll 4
+      for (int p = slice; p < n; p += slices) {
+        const float4 y = *reinterpret_cast<const float4*>(b.part + (index * b.parts + at(p)) * b.d + 4 * unit);
+        const float f = query_factor(stat[at(p)].x, top);
+        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+      }
     }
+    sums[tid] = x;
+    if constexpr (LANES == kJoinThreads) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    if (slice == 0) {
+      for (int p = 1; p < slices; ++p) {
+        const float4 y = sums[tid - u + p * units + unit];
+        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+      }
+      const float f = total == 0.f ? 0.f : 1.f / total;
+      char* out = b.out + token * b.out_stride + ((long long)head * b.d + 4 * unit) * ES;
+      if constexpr (DT == 0) *reinterpret_cast<float4*>(out) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+      else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<DT>(x.x * f, x.y * f), pack2<DT>(x.z * f, x.w * f));
+    }
+    if constexpr (LANES != kJoinThreads) __builtin_amdgcn_wave_barrier();
   }
-  sums[tid] = x;
-  __syncthreads();
-  if (slice != 0) return;
-  for (int i = 1; i < slices; ++i) {
-    const float4 y = sums[i * units + unit];
-    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-  }
-  const float f = total == 0.f ? 0.f : 1.f / total;
-  char* out = b.out + token * b.out_stride + ((long long)head * b.d + 4 * unit) * ES;
-  if constexpr (DT == 0) *reinterpret_cast<float4*>(out) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
-  else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<DT>(x.x * f, x.y * f), pack2<DT>(x.z * f, x.w * f));
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------
+
+// In blocks of 64 keys (2 us): a workgroup's beginning and end, a second launch, a channel of a part written and read again.
+constexpr double kEnds = 3, kJoin = 2, kPart = 5e-7;
 
 // How the keys of one kind of segment are cut.
 struct Cut {
@@ -83,14 +97,37 @@ struct Cut {
 Cut make_cut(int64_t tokens, int group, int segments, int kv_heads, int64_t max_len, int d, int es) {
   Cut c{false, 64, 1};
   if (segments < 1) return c;
-  const int64_t rows = tokens * group;
-  c.few = rows <= (int64_t)kRowTile * segments && query_row_bytes(d, es) <= 512;
-  const int64_t tiles = (rows / query_tile(c.few) + std::min<int64_t>(segments, rows)) * kv_heads;
-  const int least = c.few ? 256 : 512;
-  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / std::max<int64_t>(tiles, 1), (max_len + least - 1) / least, 512}));
-  const int64_t chunk = ((max_len + chunks - 1) / chunks + 127) / 128 * 128;
-  c.chunk = (int)std::max<int64_t>(chunk, 128);
-  c.chunks = (int)std::max<int64_t>(1, (max_len + c.chunk - 1) / c.chunk);
+  const int64_t rows = tokens * group, row_bytes = query_row_bytes(d, es);
+  c.few = rows <= (int64_t)kRowTile * segments && row_bytes <= 1024;
+  // Workgroups of one chunk each: at most one a tile more than the rows fill, and a compute unit holds two (few rows, wide rows: one).
+  const int64_t tiles = (rows / query_tile(c.few) + std::min<int64_t>(segments, rows)) * kv_heads, slots = row_bytes > 512 || (!c.few && row_bytes > 256) ? 256 : 512;
+  if (c.few) {
+    // Bound by memory and by how even the load is: chunks of 1,024 keys, shorter ones where those would not make three or four rounds (whole calls by
+    // 256 / 512 / 1,024 / 2,048, us: 32 sequences of 1,013 to 8,117 keys, 64 heads on 8 of 128 bf16 channels 125 / 110 / 106 / 119; 5 of 333 to 4,979,
+    // 16 heads of 72, fp32 85 / 91 / 109 / 204); one for short ones, where a second launch costs more than blocks that follow each other (257
+    // keys 10.0, as two chunks 13.1).
+    c.chunk = 1024;
+    while (c.chunk > 256 && tiles * ((max_len + c.chunk - 1) / c.chunk) < 1800) c.chunk /= 2;
+    if (max_len <= 512) c.chunk = 512;
+    c.chunks = (int)std::max<int64_t>(1, (max_len + c.chunk - 1) / c.chunk);
+    return c;
+  }
+  // The cut with the least time, in units of a block of 64 keys: workgroups in rounds (one length), or all their work dealt out and the longest one
+  // behind it (lengths of half the largest on average), each with a beginning and an end; a second launch, and what it takes for each part of a row.
+  const int64_t blocks = (max_len + 63) / 64;
+  double best = 0;
+  for (int64_t n = 1; n <= std::min<int64_t>(blocks, 256); ++n) {
+    const int64_t chunk = (blocks + n - 1) / n;
+    if ((blocks + chunk - 1) / chunk != n) continue;      // (as many blocks each as with fewer)
+    const double work = (double)tiles * n * (chunk + kEnds) / slots;
+    const double time = segments == 1 ? std::ceil((double)tiles * n / slots) * (chunk + kEnds) : work / 2 + chunk + kEnds;
+    const double cost = time + (n > 1 ? kJoin + (double)rows * kv_heads * n * d * kPart : 0);
+    if (n == 1 || cost < best) {
+      best = cost;
+      c.chunk = (int)chunk * 64;
+      c.chunks = (int)n;
+    }
+  }
   return c;
 }
 
@@ -149,9 +186,6 @@ int check_rows(sttm_ctx* ctx, int dtype, int head_dim, int q_heads, int64_t toke
   return STTM_OK;
 }
 
-// Scales that the softmax can take into its exponent: no product of a difference of scores with one leaves fp32's range at either end.
-bool ordinary(float scale) { return scale >= 1e-30f && scale <= 1e30f; }
-
 Plan plan_cross(const sttm_states* s, int64_t tokens, int q_heads) {
   const Cut b = make_cut(tokens, q_heads / s->kv_heads, s->batch, s->kv_heads, std::min<int64_t>(s->max_rows, s->rows), s->head_dim, elem_bytes(s->dtype));
   return make_plan(Cut{false, 1, 0}, b, tokens, q_heads, s->head_dim);
@@ -167,7 +201,10 @@ Plan plan_shared(const sttm_cache* c, const sttm_sequences* prefixes, const sttm
 template <int DT> void launch_all(QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb, const Plan& p, hipStream_t s) {
   if (p.a.chunks) launch_queries<DT>(a, ka, p.a.few, s);
   launch_queries<DT>(b, kb, p.b.few, s);
-  if (p.parts > 1) hipLaunchKernelGGL((k_query_join<DT>), dim3((unsigned)b.tokens, b.kv_heads * b.group), dim3(kJoinThreads), 0, s, a, ka, b, kb);
+  if (p.parts < 2) return;
+  const unsigned tokens = (unsigned)b.tokens, heads = b.kv_heads * b.group, some = kJoinHeads * (kJoinThreads / kWave);
+  if ((int64_t)tokens * heads < kJoinWaves) hipLaunchKernelGGL((k_query_join<DT, kJoinThreads>), dim3(tokens, heads), dim3(kJoinThreads), 0, s, a, ka, b, kb);
+  else hipLaunchKernelGGL((k_query_join<DT, kWave>), dim3(tokens, (heads + some - 1) / some), dim3(kJoinThreads), 0, s, a, ka, b, kb);
 }
 
 int launch(sttm_ctx* ctx, int dtype, QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb, const Plan& p, char* ws) {
@@ -178,6 +215,7 @@ int launch(sttm_ctx* ctx, int dtype, QueryArgs a, KeyArgs ka, QueryArgs b, KeyAr
     a.stat = b.stat = reinterpret_cast<float2*>(ws + p.stat);
   }
   a.parts = b.parts = p.parts;
+  b.alone = p.a.chunks == 0;
   a.first_part = 0;
   b.first_part = p.a.chunks;
   ka.chunk = p.a.chunk; ka.chunks = p.a.chunks;
@@ -207,7 +245,7 @@ QueryArgs make_queries(int dtype, int64_t tokens, int batch, int q_heads, int kv
   return a;
 }
 
-KeyArgs make_paged(const sttm_cache* c, const sttm_sequences* s, const float* bias, int64_t slots, float scale) {
+KeyArgs make_paged(const sttm_cache* c, const sttm_sequences* s, const float* bias, int64_t slots) {
   KeyArgs k{};
   const Seqs seqs = make_seqs(c, s);
   k.pool = make_pool(c);
@@ -216,10 +254,11 @@ KeyArgs make_paged(const sttm_cache* c, const sttm_sequences* s, const float* bi
   k.table_stride = seqs.table_stride;
   k.max_len = seqs.max_len;
   k.token_stride = k.pool.token_stride;
+  k.from_each = ~0;
+  k.slot_mask = c->page_size - 1;
   k.bias = bias;
   k.bias_segment = c->kv_heads * slots;
   k.bias_head = slots;
-  k.scaled = bias || !ordinary(scale);
   return k;
 }
 
@@ -262,9 +301,9 @@ extern "C" int sttm_cross_attention(sttm_ctx* ctx, const sttm_states* states, in
   k.rows = states->rows;
   k.max_len = (int)max_len;
   k.token_stride = states->row_stride * es;
+  k.slot_mask = 0x7fffffff;
   k.bias = key_bias;
   k.bias_head = bias_stride;
-  k.scaled = key_bias || !ordinary(scale);
   return launch(ctx, states->dtype, QueryArgs{}, KeyArgs{}, b, k, p, static_cast<char*>(workspace));
 }
 
@@ -301,13 +340,13 @@ extern "C" int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, con
   if (rc != STTM_OK) return rc;
   const QueryArgs b = make_queries(cache->dtype, tokens, seqs->batch, q_heads, cache->kv_heads, cache->head_dim, scale, q, q_stride, q_offsets, out,
                                    out_stride, lse);
-  KeyArgs kb = make_paged(cache, seqs, key_bias, key_slots, scale), ka{};
+  KeyArgs kb = make_paged(cache, seqs, key_bias, key_slots), ka{};
   kb.causal = 1;
   QueryArgs a = b;
   if (p.a.chunks) {
     a.cuts = group_offsets;
     a.segments = prefixes->batch;
-    ka = make_paged(cache, prefixes, prefix_bias, prefix_slots, scale);
+    ka = make_paged(cache, prefixes, prefix_bias, prefix_slots);
   }
   return launch(ctx, cache->dtype, a, ka, b, kb, p, static_cast<char*>(workspace));
 }

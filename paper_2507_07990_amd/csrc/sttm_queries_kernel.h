@@ -3,6 +3,10 @@
 #include "sttm_queries.h"
 
 #include <cmath>
+#include <type_traits>
+
+// (for lambdas: one that is not inlined has its captures in memory)
+#define STTM_INLINE __attribute__((always_inline))
 
 namespace sttm {
 namespace {
@@ -36,6 +40,11 @@ __device__ inline w2 tr_load(const char* at) {
   typedef short v4 __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(w2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4*)at));
 }
+// The larger of a lane's number and that of the lane 32 further.
+__device__ inline float of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 // Wait states between matrix products and what reads their results behind a branch (19 for the longest of them): the compiler (ROCm 7.2)
 // puts none across one.
 __device__ inline void settle() {
@@ -44,11 +53,16 @@ __device__ inline void settle() {
   __builtin_amdgcn_sched_barrier(0);
 }
 // Sixteen bytes from memory to LDS, past the registers: lane i's to base + 16 i (base the same in all lanes). Lanes that do not take part leave
-// their place as it is. arrived(): all of this wavefront's are there.
+// their place as it is. arrived(): all of this wavefront's are there but the last LATER loads.
 __device__ inline void to_lds(const char* from, char* base) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)base, 16, 0, 0);
 }
-__device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int LATER> __device__ inline void arrived() {
+  static_assert(LATER < 64, "a counter of six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LATER & 15) | 7 << 4 | 15 << 8 | (LATER >> 4) << 14);  // (the other counters as they are)
+  asm volatile("" ::: "memory");
+}
 #else
 struct EmulTiles { w4 a[64], b[64]; };
 inline EmulTiles& emul_tiles() {
@@ -98,9 +112,11 @@ inline w2 tr_load(const char* at) {
   return r;
 }
 inline void settle() {}
+inline float of_halves(float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); }
 inline void to_lds(const char* from, char* base) { memcpy(base + 16 * (threadIdx.x & 63), from, 16); }
-inline void arrived() {}
+template <int LATER> inline void arrived() {}
 #define __builtin_amdgcn_sched_barrier(x) ((void)0)
+#define __builtin_amdgcn_sched_group_barrier(kinds, count, group) ((void)0)
 #define __builtin_amdgcn_readlane(x, i) __shfl(x, i)
 #endif
 
@@ -119,16 +135,18 @@ template <int DT> __device__ inline uint32_t finite_only(uint32_t x) {
   return ((x & E) == E ? 0u : x & 0xffffu) | ((x >> 16 & E) == E ? 0u : x & 0xffff0000u);
 }
 
+__device__ __align__(16) const char kZeros[16] = {};
+
 // How a workgroup is made up: wavefronts (two buffers each have to fit LDS where a wavefront has blocks of its own), keys of a block, sixteen-byte
 // pieces that a thread brings of it.
 constexpr int query_waves(int dt, int dp, bool few) { return few && query_row_bytes(dp, dt == 0 ? 4 : 2) > 256 ? 2 : kQueryWaves; }
-constexpr int query_blocks_a_unit(int dt, int dp, bool few) { return few || query_row_bytes(dp, dt == 0 ? 4 : 2) > 256 ? 1 : 2; }
+constexpr int query_waves_a_simd(int dt, int dp) { return dp * (dt == 0 ? 4 : 2) > 256 ? 1 : 2; }
 template <int DT, int DP, bool FEW> struct Shape {
   static constexpr int ES = DT == 0 ? 4 : 2, M = DP / 32, NQ = DP * ES / 32;
   static constexpr int ROW = query_row_bytes(DP, ES), CH = ROW / 16;
   static constexpr int WAVES = query_waves(DT, DP, FEW), THREADS = WAVES * kWave;
   static constexpr int SHARE = FEW ? 1 : WAVES;           // wavefronts that share a block of keys
-  static constexpr int SETS = WAVES / SHARE;
+  static constexpr int SETS = WAVES / SHARE, BUFFERS = FEW ? 1 : 2;
   static constexpr int NK = !FEW && ROW <= 256 ? 64 : 32, KT = NK / 32;
   static constexpr int AT_ONCE = kWave / CH;              // rows of one load of a wavefront
   static constexpr int PER = NK / (AT_ONCE * SHARE);      // loads of a wavefront for a block's keys
@@ -146,18 +164,21 @@ template <int DT, int DP, bool FEW> struct Shape {
 // P is rounded to 16 bits for 16-bit values (half a step of the type: as much as the rounding of the result, which the sum over keys
 // mostly averages away); the sum that divides is that of the unrounded ones, in 32 bits. In fp16 it is 2^15 P, so that a weight is
 // off by no more than 2^-40 of the largest one where fp16 runs out of exponents.
-template <int DT, int DP, bool FEW>
-__global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks_a_unit(DT, DP, FEW)) k_query_tiles(QueryArgs a, KeyArgs kk) {
+template <int DT, int DP, bool FEW, bool CAUSAL, bool FULL>
+__global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_a_simd(DT, DP)) k_query_tiles(QueryArgs a, KeyArgs kk) {
   using S = Shape<DT, DP, FEW>;
-  constexpr int ES = S::ES, ROW = S::ROW, CH = S::CH, NQ = S::NQ, M = S::M, SETS = S::SETS, NK = S::NK, KT = S::KT;
-  constexpr int AT_ONCE = S::AT_ONCE, PER = S::PER, TILE = S::TILE, THREADS = S::THREADS;
+  constexpr int ES = S::ES, ROW = S::ROW, CH = S::CH, NQ = S::NQ, M = S::M, SETS = S::SETS, BUFFERS = S::BUFFERS, NK = S::NK, KT = S::KT;
+  constexpr int AT_ONCE = S::AT_ONCE, PER = S::PER, TILE = S::TILE;
   constexpr float LIFT = DT == 2 ? 15.f : 0.f;
   constexpr float UNLIFT = DT == 2 ? 1.f / 32768.f : 1.f;
-  constexpr bool WIDE = DP * ES > 256;                    // one way for all blocks: the registers that two ways take are not there
-  static_assert(CH >= 8 && CH <= 64 && NK % (AT_ONCE * S::SHARE) == 0 && (!FEW || SETS * 2 * NK * ROW * 2 >= S::WAVES * 4096), "tiles");
+  constexpr int K_AHEAD = DT == 0 ? 2 : 4, V_AHEAD = 2;  // pieces of keys, steps of values read ahead
+  constexpr bool ONE_WAY = DP * ES > 256;                 // (the registers that two ways take are not there)
+  static_assert(CH >= 8 && CH <= 64 && NK % (AT_ONCE * S::SHARE) == 0 && (!FEW || SETS * NK * ROW >= S::WAVES * 4096), "tiles");
 
-  __shared__ __align__(16) char tiles[SETS][2][2][NK * ROW];  // of each set two buffers of keys and of values
-  __shared__ __align__(16) float adds[SETS][2][NK];       // what is added to a key's score: its bias; -inf: it does not count
+  // Keys and values, two buffers where wavefronts share them. (Arrays of their own: the compiler waits for all loads to LDS before it reads what they
+  // might have written to.)
+  __shared__ __align__(16) char keys0[SETS * NK * ROW], values0[SETS * NK * ROW], keys1[BUFFERS == 2 ? NK * ROW : 16], values1[BUFFERS == 2 ? NK * ROW : 16];
+  __shared__ __align__(16) float adds[SETS][BUFFERS][NK];  // what is added to a key's score: its bias; -inf: it does not count
   __shared__ float stat_m[SETS][kRowTile], stat_l[SETS][kRowTile];
   __shared__ int odd_value;                               // a value that is not finite in a block whose keys not all rows see
 
@@ -181,7 +202,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
   const long long in_row = min(row, rows - 1), in_token = in_row / a.group, token = token0 + in_token;
   const int head = h * a.group + (int)(in_row - in_token * a.group);
   int limit = length, end = min(length, first + kk.chunk), least = length;   // slots that the row, any row of the tile, all of them see
-  if (kk.causal) {
+  if constexpr (CAUSAL) {
     const long long behind = length - rows / a.group + 1;
     limit = (int)max(behind + in_token, 0ll);
     least = (int)max(behind + row0 / a.group, 0ll);
@@ -202,58 +223,49 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
 
   const float* bias = kk.bias ? kk.bias + s * kk.bias_segment + h * kk.bias_head + key0 : nullptr;
   const int32_t* table = kk.table ? kk.table + s * kk.table_stride : nullptr;
-  const int page_mask = (1 << kk.pool.shift) - 1;
   const long long base = h * kk.pool.head_stride + key0 * kk.token_stride;
   const int stride = (int)kk.token_stride;                // (a block's rows lie within 2 GiB)
 
   // The pieces of LDS that this lane fills with load i: of row brought + AT_ONCE * SHARE * i (+ its own row of the AT_ONCE of a load), which lie
   // in one page. Pieces behind a head's channels stay zero.
   const int brought = __builtin_amdgcn_readfirstlane(share * AT_ONCE), own_row = lane / CH;
-  int key_from[PER], value_from[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int r = brought + AT_ONCE * S::SHARE * i + own_row;
-    key_from[i] = 16 * (lane % CH ^ key_order<CH>(r));
-    value_from[i] = 16 * (lane % CH ^ value_order<DT, CH>(r));
-  }
-  const bool full = kk.pool.row == ROW;
-  // Lane i: the page of the block's key i, looked up a block ahead, and what is added to its score. Keys from the end on: the page of the
-  // last one, whose other slots may be read.
-  int page_next = 0;
-  float add_next = 0.f;
-  auto look_up = [&](int s0) {
-    if (table) page_next = table[min(s0 + min(lane, NK - 1), end - 1) >> kk.pool.shift];
+  auto key_from = [&](int i) STTM_INLINE { return 16 * (lane % CH ^ key_order<CH>(brought + AT_ONCE * S::SHARE * i + own_row)); };
+  auto value_from = [&](int i) STTM_INLINE { return 16 * (lane % CH ^ value_order<DT, CH>(brought + AT_ONCE * S::SHARE * i + own_row)); };
+  // Lane i: the page of key i of the block that is loaded next and its bias, looked up a block ahead; of the block on its way, what is added to the
+  // key's score. Keys from the end on: the page of the last one, whose other slots may be read.
+  int page_next = 0, page_now = 0;                        // (packed: 0)
+  float bias_next = 0.f, add_now = 0.f;
+  auto look_up = [&](int s0) STTM_INLINE {
+    const int slot = min(s0 + min(lane, NK - 1), end - 1);
+    if (table) page_next = table[slot >> kk.pool.shift];
+    if (bias) bias_next = bias[slot];
   };
-  auto load = [&](int s0, int buffer) {
+  auto next_block = [&](int s0) STTM_INLINE {
     const bool there = !table || (unsigned)page_next < (unsigned)kk.pool.pages;
-    add_next = bias ? bias[min(s0 + min(lane, NK - 1), end - 1)] : 0.f;
-    if (lane >= NK || s0 + lane >= end || !there) add_next = -INFINITY;
-    const int page = there ? page_next : 0;               // (what is read of a page that is not there does not count)
-    char* const to = tiles[set][buffer][0] + brought * ROW;
+    add_now = lane >= NK || s0 + lane >= end || !there ? -INFINITY : bias_next;
+    page_now = there ? page_next : 0;                     // (what is read of a page that is not there does not count)
+  };
+  // (As many loads whatever the width and the source, one after the other, for the sake of those that count them: pieces behind a head's channels
+  // come from a place of zeros. Pages: each load from the start of its rows. Packed: from the block's first row, rows from the end on the last one.)
+  const int each = kk.from_each, slot_mask = kk.slot_mask;
+  const unsigned long long page_stride = kk.pool.page_stride;
+  const int own_from = own_row * stride;
+  auto load = [&](auto what, int s0, char* keys_to, char* values_to) STTM_INLINE {
+    constexpr bool KEYS = decltype(what)::value & 1, VALUES = decltype(what)::value & 2;
+    const int at_lds = (set * NK + brought) * ROW, last = kk.table ? 0x7fffffff : min(end - 1 - s0, NK) * stride;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int r = brought + AT_ONCE * S::SHARE * i;
-      long long from;
-      int row = own_row * stride;
-      if (table) {
-        from = __builtin_amdgcn_readlane(page, r) * kk.pool.page_stride + base + ((s0 + r) & page_mask) * stride;
-      } else {
-        from = base + (s0 + r) * kk.token_stride;
-        if (s0 + NK > end) {                              // (rows from the end on: the last one)
-          from = base + s0 * kk.token_stride;
-          row = min(r + own_row, end - 1 - s0) * stride;
-        }
-      }
-      char* const at = to + AT_ONCE * S::SHARE * i * ROW;
-      if (full) {
-        to_lds(kk.pool.k + from + (unsigned)(row + key_from[i]), at);
-        to_lds(kk.pool.v + from + (unsigned)(row + value_from[i]), at + NK * ROW);
-      } else {
-        if (key_from[i] < kk.pool.row) to_lds(kk.pool.k + from + (unsigned)(row + key_from[i]), at);
-        if (value_from[i] < kk.pool.row) to_lds(kk.pool.v + from + (unsigned)(row + value_from[i]), at + NK * ROW);
-      }
+      const int r = brought + AT_ONCE * S::SHARE * i, at = at_lds + AT_ONCE * S::SHARE * i * ROW;
+      const long long from = base + (unsigned)__builtin_amdgcn_readlane(page_now, r) * page_stride + (unsigned long long)(unsigned)((s0 + (r & each)) & slot_mask) * (unsigned)stride;
+      const unsigned row = (unsigned)min(own_from + (r & ~each) * stride, last);
+      const char *k_from = kk.pool.k + from, *v_from = kk.pool.v + from;
+      if constexpr (KEYS) to_lds(FULL || key_from(i) < kk.pool.row ? k_from + (row + key_from(i)) : kZeros, keys_to + at);
+      if constexpr (VALUES) to_lds(FULL || value_from(i) < kk.pool.row ? v_from + (row + value_from(i)) : kZeros, values_to + at);
     }
   };
+  using Keys = std::integral_constant<int, 1>;
+  using Values = std::integral_constant<int, 2>;
+  using Both = std::integral_constant<int, 3>;
 
   // Where this lane reads in LDS: the parts of an address that rows of a fixed distance have in common.
   constexpr int P = CH >= 16 ? 16 : 8, NK_AT = NQ < P / 2 ? NQ : P / 2, NV_AT = DT != 0 ? M : M < 2 || CH < 16 ? 1 : 2;
@@ -274,92 +286,109 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
   for (int n = 0; n < M; ++n)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[n][r] = 0.f;
-  // Scores that have no bias stay as the product gives them, the scale is part of the exponent's factor.
-  constexpr float kWide = 65536.f;                        // (times 2^-24 is what the rounding of `from` may leave in an exponent)
   float m = -INFINITY, from = 0.f, l = 0.f;  // from: m as an exponent of two; l: of this lane's keys
-  const float times = kk.scaled ? kLog2e : a.scale * kLog2e, scaled = kk.scaled ? a.scale : 1.f;
   if (tid == 0) odd_value = 0;
-  if (!full) {                                            // pieces of LDS that nothing is loaded into
-    for (int i = tid; i < (int)sizeof(tiles) / 16; i += THREADS) reinterpret_cast<w4*>(tiles)[i] = w4{0u, 0u, 0u, 0u};
-    __syncthreads();
-  }
   const int start = first + set * NK, step = SETS * NK;
   if (start < end) {
     look_up(start);
-    load(start, 0);
+    next_block(start);
+    if constexpr (FEW) load(Keys(), start, keys0, values0);
+    else load(Both(), start, keys0, values0);
     look_up(start + step);
+    if constexpr (FEW) load(Values(), start, keys0, values0);
   }
-  int buffer = 0;
-  for (int s0 = start; s0 < end; s0 += step, buffer ^= 1) {
-    char* const keys = tiles[set][buffer][0];
-    char* const values = tiles[set][buffer][1];
-    arrived();
-    const unsigned long long alive = __ballot(add_next != -INFINITY);
-    const bool whole = alive == (NK == 64 ? ~0ull : 0xffffffffull);
-    const bool diagonal = s0 + NK > least && least < length, added = WIDE || kk.scaled || !whole;
-    if (diagonal || !whole) {                             // (this wavefront's own pieces: it sees what it loaded)
-      __builtin_amdgcn_wave_barrier();
-      bool odd = false;
+  arrived<0>();                                           // (the queries, too, which the compiler would wait for with every block else)
+  // A block's keys (values) that count for none of the rows, or values that are not finite where not all rows see them: nothing of those may be
+  // infinite or NaN. Each wavefront sees to the pieces that it has loaded.
+  auto mend = [&](char* at, unsigned long long alive, bool finite) STTM_INLINE {
+    bool odd = false;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int r = brought + AT_ONCE * S::SHARE * i;
-        w4* at = reinterpret_cast<w4*>(values + r * ROW + 16 * lane);
-        if (!(alive >> (r + own_row) & 1)) {              // a key that does not count: nothing of it may be infinite or NaN
-          *at = w4{0u, 0u, 0u, 0u};
-          *reinterpret_cast<w4*>(keys + r * ROW + 16 * lane) = w4{0u, 0u, 0u, 0u};
-        } else if (diagonal) {
-          w4 y = *at;
+    for (int i = 0; i < PER; ++i) {
+      const int r = brought + AT_ONCE * S::SHARE * i;
+      w4* piece = reinterpret_cast<w4*>(at + r * ROW + 16 * lane);
+      if (!(alive >> (r + own_row) & 1)) {
+        *piece = w4{0u, 0u, 0u, 0u};
+      } else if (finite) {
+        w4 y = *piece;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t f = finite_only<DT>(y[e]);
-            odd |= f != y[e];
-            y[e] = f;
-          }
-          *at = y;
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t f = finite_only<DT>(y[e]);
+          odd |= f != y[e];
+          y[e] = f;
         }
+        *piece = y;
       }
-      if (odd) odd_value = 1;
     }
-    if (share == 0 && lane < NK && added) adds[set][buffer][lane] = add_next;
-    if constexpr (FEW) __builtin_amdgcn_wave_barrier();
-    else __syncthreads();
-    if (s0 + step < end) {
-      load(s0 + step, buffer ^ 1);
-      look_up(s0 + 2 * step);
-    }
-
+    if (odd) odd_value = 1;
+  };
+  // One block. FEW: a wavefront has its block to itself, one buffer for keys and one for values; the next keys are on their way from the first
+  // product on, the next values from the second.
+  auto block = [&](int s0, bool more, bool diagonal, bool whole, unsigned long long alive, const char* keys, char* values, const float* added) STTM_INLINE {
+    // S^T. The pieces of keys are read a few products ahead (a read takes as long as four of them).
     f32x16 x[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[t][r] = 0.f;
-#pragma unroll
-    for (int c = 0; c < NQ; ++c) {
-      if (DP * ES > 256 && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // (not all reads before the first product: registers)
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        const w4 k = *reinterpret_cast<const w4*>(keys + key_at[c % NK_AT] + (32 * t * ROW + c / NK_AT * NK_AT * 32));
-        if constexpr (DT == 0) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[t] = mma32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), x[t]);
-        } else {
-          x[t] = mma16<DT>(k, q[c], x[t]);
-        }
-      }
-    }
-    settle();
-    if (added) {
+    w4 k[K_AHEAD][KT];
+    auto read_keys = [&](int c) STTM_INLINE {
 #pragma unroll
       for (int t = 0; t < KT; ++t)
+        k[c % K_AHEAD][t] = *reinterpret_cast<const w4*>(keys + key_at[c % NK_AT] + (32 * t * ROW + c / NK_AT * NK_AT * 32));
+    };
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const float4 add = *reinterpret_cast<const float4*>(&adds[set][buffer][32 * t + 8 * r4 + 4 * g]);
-          const float of[4] = {add.x, add.y, add.z, add.w};
+    for (int c = 0; c < K_AHEAD; ++c) read_keys(c);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[t][4 * r4 + e] = fmaf(x[t][4 * r4 + e], scaled, of[e]);
+    for (int c = 0; c < NQ; ++c) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        if constexpr (DT == 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[t] = mma32(__uint_as_float(k[c % K_AHEAD][t][e]), __uint_as_float(q[c][e]), x[t]);
+        } else {
+          x[t] = mma16<DT>(k[c % K_AHEAD][t], q[c], x[t]);
         }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (c + K_AHEAD < NQ) read_keys(c + K_AHEAD);
     }
-    if (diagonal) {
+    // Values, the first ones on their way while the softmax goes on: of step j the keys that one product takes (16, fp32: 1 a half).
+    constexpr int STEPS = DT == 0 ? 16 * KT : NK / 16;
+    w4 v[V_AHEAD][DT == 0 ? (M + 3) / 4 : M];
+    auto read_values = [&](int j) STTM_INLINE {
+#pragma unroll
+      for (int n = 0; n < M; ++n) {
+        if constexpr (DT == 0) {
+          const char* at = values + value_at[n % NV_AT] + ((8 * (j / 4) + j % 4) * ROW + n / NV_AT * NV_AT * 128);
+          v[j % V_AHEAD][n / 4][n % 4] = *reinterpret_cast<const uint32_t*>(at);
+        } else {
+          const w2 lo = tr_load(values + value_at[n] + 16 * j * ROW), hi = tr_load(values + value_at[n] + (16 * j + 8) * ROW);
+          v[j % V_AHEAD][n] = w4{lo[0], lo[1], hi[0], hi[1]};
+        }
+      }
+    };
+    if constexpr (FEW) {
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_wave_barrier();
+      if (more) {
+        next_block(s0 + step);
+        load(Keys(), s0 + step, keys0, values0);
+      }
+    } else {
+      read_values(0);
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const float4 add = *reinterpret_cast<const float4*>(&added[32 * t + 8 * r4 + 4 * g]);
+        x[t][4 * r4] = fmaf(x[t][4 * r4], a.scale, add.x);
+        x[t][4 * r4 + 1] = fmaf(x[t][4 * r4 + 1], a.scale, add.y);
+        x[t][4 * r4 + 2] = fmaf(x[t][4 * r4 + 2], a.scale, add.z);
+        x[t][4 * r4 + 3] = fmaf(x[t][4 * r4 + 3], a.scale, add.w);
+      }
+    if (CAUSAL && diagonal) {
 #pragma unroll
       for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -371,65 +400,121 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[t][r]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    if (__ballot(top > m) != 0) {  // (seldom after the first blocks)
-      const float before = m, from_before = m == -INFINITY ? -INFINITY : from;
-      m = fmaxf(m, top);
-      from = m == -INFINITY ? 0.f : m * times;
-      const float shrink = exp2_fast(fabsf(from) < kWide ? from_before - from : (before - m) * times);
-      l *= shrink;
-#pragma unroll
-      for (int n = 0; n < M; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[n][r] *= shrink;
-    }
+    top = of_halves(top);
+    const bool rises = __ballot(top > m) != 0;            // (seldom after the first blocks)
+    const float before = m, from_before = m == -INFINITY ? -INFINITY : from;
+    m = fmaxf(m, top);
+    from = m == -INFINITY ? 0.f : m * kLog2e;
+    // Large scores: no multiple of theirs, only of their differences. (A rounding of `from` times 2^-24 is what an exponent may be off else.)
     float less = LIFT - from;
-    if (WIDE || __ballot(!(fabsf(from) < kWide)) != 0) {  // large scores: no multiple of theirs, only of their differences
+    if (ONE_WAY || __ballot(!(fabsf(from) < 65536.f)) != 0) {
       less = LIFT;
 #pragma unroll
       for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[t][r] -= m == -INFINITY ? 0.f : m;
     }
+    if (rises) {
+      const float by = exp2_fast(fabsf(from) < 65536.f ? from_before - from : (before - m) * kLog2e);
+      l *= by;
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+      for (int n = 0; n < M; ++n)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[t][r] = exp2_fast(fmaf(x[t][r], times, less));
-        l += x[t][r];
+        for (int r = 0; r < 16; ++r) acc[n][r] *= by;
+    }
+    if constexpr (FEW) {
+      if (more) arrived<PER>();                   // (all but the keys that come next)
+      else arrived<0>();
+      if (diagonal || !whole) {
+        __builtin_amdgcn_wave_barrier();
+        mend(values, alive, diagonal);
       }
-    if constexpr (DT == 0) {
+      __builtin_amdgcn_wave_barrier();
+      read_values(0);
+    }
+    // O^T, the exponentials of a step while the products of the one before it go on.
+    constexpr int EACH = DT == 0 ? 1 : 8;                 // scores a lane has of one step
+    w4 p[2];
+    auto weigh = [&](int j) STTM_INLINE {
 #pragma unroll
-      for (int t = 0; t < KT; ++t)
+      for (int e = 0; e < EACH; ++e) {
+        const int at = j * EACH % 16 + e;
+        x[j * EACH / 16][at] = exp2_fast(fmaf(x[j * EACH / 16][at], kLog2e, less));
+        l += x[j * EACH / 16][at];
+      }
+      if constexpr (DT != 0) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if (r % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        for (int w = 0; w < 4; ++w) p[j % 2][w] = pack2<DT>(x[j / 2][8 * (j % 2) + 2 * w], x[j / 2][8 * (j % 2) + 2 * w + 1]);
+      }
+    };
+    weigh(0);
 #pragma unroll
-          for (int n = 0; n < M; ++n) {
-            const char* at = values + value_at[n % NV_AT] + ((32 * t + 8 * (r / 4) + r % 4) * ROW + n / NV_AT * NV_AT * 128);
-            acc[n] = mma32(*reinterpret_cast<const float*>(at), x[t][r], acc[n]);
-          }
-        }
+    for (int j = 0; j < STEPS; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (j + 1 < STEPS) read_values(j + 1);
+#pragma unroll
+      for (int n = 0; n < M; ++n) {
+        if constexpr (DT == 0) acc[n] = mma32(__uint_as_float(v[j % V_AHEAD][n / 4][n % 4]), x[j / 16][j % 16], acc[n]);
+        else acc[n] = mma16<DT>(v[j % V_AHEAD][n], p[j % 2], acc[n]);
+      }
+      if (j + 1 < STEPS) weigh(j + 1);
+      // (reads, then a product and what two of the next step's scores take, in turn)
+      __builtin_amdgcn_sched_group_barrier(0x100, DT == 0 ? M : 2 * M, 0);
+#pragma unroll
+      for (int n = 0; n < M; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, DT == 0 ? 4 : (28 + M - 1) / M, 0);
+      }
+    }
+  };
+  auto one = [&](int s0, char* keys, char* values, char* next_keys, char* next_values, float* added) STTM_INLINE {
+    keys += set * NK * ROW;
+    values += set * NK * ROW;
+    const bool more = s0 + step < end;
+    if (FEW) arrived<PER>();                              // (all but the values)
+    else arrived<0>();
+    const unsigned long long alive = __ballot(add_now != -INFINITY);
+    const bool whole = alive == (NK == 64 ? ~0ull : 0xffffffffull);
+    const bool diagonal = CAUSAL && s0 + NK > least && least < length;
+    if (diagonal || !whole) {
+      __builtin_amdgcn_wave_barrier();
+      if (!whole) mend(keys, alive, false);
+      if (!FEW) mend(values, alive, diagonal);
+    }
+    if (share == 0 && lane < NK) added[lane] = add_now;
+    if constexpr (FEW) {
+      __builtin_amdgcn_wave_barrier();
     } else {
-#pragma unroll
-      for (int j = 0; j < NK / 16; ++j) {
-        __builtin_amdgcn_sched_barrier(0);
-        w4 p;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) p[w] = pack2<DT>(x[j / 2][8 * (j % 2) + 2 * w], x[j / 2][8 * (j % 2) + 2 * w + 1]);
-#pragma unroll
-        for (int n = 0; n < M; ++n) {
-          const w2 lo = tr_load(values + value_at[n] + 16 * j * ROW), hi = tr_load(values + value_at[n] + (16 * j + 8) * ROW);
-          acc[n] = mma16<DT>(w4{lo[0], lo[1], hi[0], hi[1]}, p, acc[n]);
-        }
+      __syncthreads();
+      if (more) {
+        next_block(s0 + step);
+        load(Both(), s0 + step, next_keys, next_values);
+        look_up(s0 + 2 * step);
       }
+    }
+    block(s0, more, diagonal, whole, alive, keys, values, added);
+    if constexpr (FEW) {
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_wave_barrier();
+      if (more) {
+        look_up(s0 + 2 * step);
+        load(Values(), s0 + step, keys0, values0);
+      }
+    }
+  };
+  if constexpr (FEW) {
+    for (int s0 = start; s0 < end; s0 += step) one(s0, keys0, values0, nullptr, nullptr, adds[set][0]);
+  } else {
+    for (int s0 = start; s0 < end; s0 += 2 * step) {
+      one(s0, keys0, values0, keys1, values1, adds[0][0]);
+      if (s0 + step < end) one(s0 + step, keys1, values1, keys0, values0, adds[0][BUFFERS - 1]);
     }
   }
   settle();
 
+  const bool parted = a.part && !(a.alone && length <= kk.chunk);
   l += __shfl_xor(l, 32, 64);
   l *= UNLIFT;
-  if (!kk.scaled && m != -INFINITY) m *= a.scale;
   float top = m, total = l, mine_of = UNLIFT;
   if constexpr (FEW) {  // the wavefronts on a common maximum
     if (lane < kRowTile) {
@@ -444,13 +529,13 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
   }
   const long long index = token * (a.kv_heads * a.group) + head;
   if (mine && g == 0 && set == 0) {
-    if (a.part) a.stat[index * a.parts + a.first_part + chunk] = make_float2(top, total);
+    if (parted) a.stat[index * a.parts + a.first_part + chunk] = make_float2(top, total);
     else if (a.lse) a.lse[index] = top + logf(total);
   }
-  const float inverse = a.part ? 1.f : total == 0.f ? 0.f : 1.f / total;
-  float* part = a.part ? a.part + (index * a.parts + a.first_part + chunk) * a.d : nullptr;
-  char* out = a.part ? nullptr : a.out + token * a.out_stride + (long long)head * a.d * ES;
-  auto store = [&](int c, float4 y) {                     // four channels of this lane's row
+  const float inverse = parted ? 1.f : total == 0.f ? 0.f : 1.f / total;
+  float* part = parted ? a.part + (index * a.parts + a.first_part + chunk) * a.d : nullptr;
+  char* out = parted ? nullptr : a.out + token * a.out_stride + (long long)head * a.d * ES;
+  auto store = [&](int c, float4 y) STTM_INLINE {                     // four channels of this lane's row
     if (part) {
       *reinterpret_cast<float4*>(part + c) = y;
     } else {
@@ -469,7 +554,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       }
   } else {
     // 32 channels at a time: every wavefront leaves its four runs of four channels a lane, wavefront w adds the runs w, w + SETS .. up.
-    float4* joined = reinterpret_cast<float4*>(tiles);    // [wave][j][lane]
+    float4* joined = reinterpret_cast<float4*>(keys0);    // [wave][j][lane]
 #pragma unroll
     for (int n = 0; n < M; ++n) {
       __syncthreads();
@@ -490,8 +575,8 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       }
     }
   }
-  if (kk.causal) __syncthreads();                         // (odd_value, of all wavefronts)
-  if (kk.causal && odd_value) {
+  if constexpr (CAUSAL) __syncthreads();                         // (odd_value, of all wavefronts)
+  if (CAUSAL && odd_value) {
     // Values that are not finite were left out where some rows see them and others do not (a weight of zero does not make them
     // zero): the rows that see them get them here. What is infinite or NaN already stays so.
 #pragma unroll 1
@@ -501,7 +586,8 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
       for (int i = max(first, least - NK + 1); i < min(end, limit); ++i) {
         const int page = table ? table[i >> kk.pool.shift] : 0;
         if ((table && (unsigned)page >= (unsigned)kk.pool.pages) || (bias && bias[i] == -INFINITY)) continue;
-        const long long at = base + (table ? page * kk.pool.page_stride + (i & page_mask) * stride : i * kk.token_stride);
+        const long long at = base + (table ? page * kk.pool.page_stride + (i & slot_mask) * stride : i * kk.token_stride);
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
           float v;
           if constexpr (DT == 0) v = *reinterpret_cast<const float*>(kk.pool.v + at + 4 * (c + e));
@@ -509,41 +595,40 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_blocks
           if (!(fabsf(v) < INFINITY)) add[e] += v;
         }
       }
-      for (int e = 0; e < 4; ++e) {
-        if (add[e] == 0.f) continue;
-        if (part) part[c + e] += add[e];
-        else if constexpr (DT == 0) reinterpret_cast<float*>(out)[c + e] += add[e];
-        else {
-          uint16_t* to = reinterpret_cast<uint16_t*>(out) + c + e;
-          *to = (uint16_t)pack2<DT>(low_half<DT>(*to) + add[e], 0.f);
-        }
+      float* to = part ? part : DT == 0 ? reinterpret_cast<float*>(out) : nullptr;
+      if (to) {
+        const float4 y = *reinterpret_cast<const float4*>(to + c);
+        *reinterpret_cast<float4*>(to + c) = make_float4(y.x + add[0], y.y + add[1], y.z + add[2], y.w + add[3]);
+      } else if constexpr (DT != 0) {
+        const uint2 y = *reinterpret_cast<const uint2*>(out + 2 * c);
+        *reinterpret_cast<uint2*>(out + 2 * c) = make_uint2(pack2<DT>(low_half<DT>(y.x) + add[0], high_half<DT>(y.x) + add[1]),
+                                                            pack2<DT>(low_half<DT>(y.y) + add[2], high_half<DT>(y.y) + add[3]));
       }
     }
   }
 }
 
+template <int DT, int DP, bool FEW, bool CAUSAL>
+void launch_tiles(const QueryArgs& a, const KeyArgs& k, hipStream_t s) {
+  const dim3 grid((unsigned)(a.tokens * a.group / query_tile(FEW) + a.segments), a.kv_heads, k.chunks), block(Shape<DT, DP, FEW>::THREADS);
+  if (k.pool.row == Shape<DT, DP, FEW>::ROW) hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, CAUSAL, true>), grid, block, 0, s, a, k);
+  else hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, CAUSAL, false>), grid, block, 0, s, a, k);
+}
+
 template <int DT, int DP>
-void launch_tiles(const QueryArgs& a, const KeyArgs& k, bool few, hipStream_t s) {
-  constexpr int ROW = DP * (DT == 0 ? 4 : 2);
-  const dim3 grid((unsigned)(a.tokens * a.group / query_tile(few) + a.segments), a.kv_heads, k.chunks);
-  if constexpr (ROW <= 512) {
-    if (few) {
-      hipLaunchKernelGGL((k_query_tiles<DT, DP, true>), grid, dim3(Shape<DT, DP, true>::THREADS), 0, s, a, k);
-      return;
-    }
-  }
-  hipLaunchKernelGGL((k_query_tiles<DT, DP, false>), grid, dim3(Shape<DT, DP, false>::THREADS), 0, s, a, k);
+void launch_width(const QueryArgs& a, const KeyArgs& k, bool few, hipStream_t s) {
+  if (few) k.causal ? launch_tiles<DT, DP, true, true>(a, k, s) : launch_tiles<DT, DP, true, false>(a, k, s);
+  else k.causal ? launch_tiles<DT, DP, false, true>(a, k, s) : launch_tiles<DT, DP, false, false>(a, k, s);
 }
 
 }  // namespace
 
 template <int DT> void launch_queries(const QueryArgs& a, const KeyArgs& k, bool few_rows, hipStream_t s) {
-  if (a.d <= 32) launch_tiles<DT, 32>(a, k, few_rows, s);
-  else if (a.d <= 64) launch_tiles<DT, 64>(a, k, few_rows, s);
-  else if (a.d <= 96) launch_tiles<DT, 96>(a, k, few_rows, s);
-  else if (a.d <= 128) launch_tiles<DT, 128>(a, k, few_rows, s);
-  else if (a.d <= 192) launch_tiles<DT, 192>(a, k, few_rows, s);
-  else launch_tiles<DT, 256>(a, k, few_rows, s);
+  if (a.d <= 64) launch_width<DT, 64>(a, k, few_rows, s);
+  else if (a.d <= 96) launch_width<DT, 96>(a, k, few_rows, s);
+  else if (a.d <= 128) launch_width<DT, 128>(a, k, few_rows, s);
+  else if (a.d <= 192) launch_width<DT, 192>(a, k, few_rows, s);
+  else launch_width<DT, 256>(a, k, few_rows, s);
 }
 
 }  // namespace sttm
