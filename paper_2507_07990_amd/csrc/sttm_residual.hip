@@ -1,6 +1,7 @@
 // What follows a block of a layer: norm of its result, gate, residual sum, and the norm before the next block, one pass over the rows.
 #include "sttm_cache.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace sttm {
@@ -42,132 +43,185 @@ template <int DT> struct Unit {
   }
 };
 
-// The sum over the lanes that have a row, the same bits in each of them.
+// The hyperbolic tangent, within three steps of fp32: its Taylor series up to a half, where the other form would lose digits, and 1 - 2 / (e^2x + 1).
+__device__ inline float tanh_of(float x) {
+  const float s = x * x, y = fabsf(x);
+  float p = -929569.f / 638512875.f;
+  p = fmaf(p, s, 21844.f / 6081075.f);
+  p = fmaf(p, s, -1382.f / 155925.f);
+  p = fmaf(p, s, 62.f / 2835.f);
+  p = fmaf(p, s, -17.f / 315.f);
+  p = fmaf(p, s, 2.f / 15.f);
+  p = fmaf(p, s, -1.f / 3.f);
+  const float far = copysignf(1.f - 2.f / (exp2_fast(y * 2.8853900817779268f) + 1.f), x);
+  return y < 0.5f ? fmaf(x * s, p, x) : far;
+}
+
+// The sum over the lanes that have a row, the same bits in each of them. of_wave: a place that no other sum of this row uses, nor the same one
+// of the next row.
 template <int LANES> __device__ inline float row_sum(float v, float* of_wave) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   if constexpr (LANES > kWave) {
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = v;
     __syncthreads();
     v = of_wave[0];
+#pragma unroll
     for (int w = 1; w < LANES / kWave; ++w) v += of_wave[w];
   }
   return v;
 }
 
-// LANES lanes (a wavefront, or all four of a workgroup) have a row, U units of 16 bytes a lane at most, kept in registers from the one
-// read to the two writes. Sums of squares are those of differences from the mean, which is known by then.
+// LANES lanes (a wavefront where rows are short, all four of a workgroup else) have a row, U units of 16 bytes a lane at most, kept in registers
+// from the one read to the two writes; so are the weights, for all the rows that the lanes come by. The next row is on its way while this one is
+// worked on. Sums of squares are those of differences from the mean, which is known by then.
+// Bound by memory: 43,264 rows of 3,584 bf16 channels with two norms and a gate are 1.24 GB in 237 us, 5.2 TB/s (a wavefront a row, its weights from the
+// caches with every row: 362). ONCE: what is written is more than the caches are good for and goes past them.
 template <int DT, int LANES, int U, bool ONCE>
 __global__ void __launch_bounds__(kResidualThreads) k_residual_norm(ResidualArgs a) {
-  constexpr int N = Unit<DT>::N;
-  __shared__ float of_wave[kResidualThreads / kWave];
+  constexpr int N = Unit<DT>::N, ROWS = kResidualThreads / LANES;
+  constexpr bool KEEP = U <= 2;                           // weights in registers, the next row ahead (where there are registers for that)
+  __shared__ float of_wave[2][4][kResidualThreads / kWave];
   const int lane = threadIdx.x & (LANES - 1);
-  const long long row = blockIdx.x * (long long)(kResidualThreads / LANES) + threadIdx.x / LANES;
-  if (row >= a.n) return;                                 // (all lanes of a row)
-  float v[U][N], f[N];
-  uint4 x[U];
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
+  auto read = [&](const char* from, int i) __attribute__((always_inline)) {
     const int at = lane + i * LANES;
-    x[i] = make_uint4(0u, 0u, 0u, 0u);
-    uint4 y = x[i];
-    if (at < a.units) {
-      x[i] = *reinterpret_cast<const uint4*>(a.x + row * a.x_stride + 16 * at);
-      if (a.y) y = *reinterpret_cast<const uint4*>(a.y + row * a.y_stride + 16 * at);
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (at < a.units) w = *reinterpret_cast<const uint4*>(from + 16 * at);
+    return w;
+  };
+  uint4 kept[5][KEEP ? U : 1];
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+#pragma unroll
+      for (int i = 0; i < U; ++i) kept[k][i] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (a.post.weight) kept[0][i] = read(a.post.weight, i);
+      if (a.post.bias) kept[1][i] = read(a.post.bias, i);
+      if (a.pre.weight) kept[2][i] = read(a.pre.weight, i);
+      if (a.pre.bias) kept[3][i] = read(a.pre.bias, i);
+      if (a.gate_wide && !a.gate_stride) kept[4][i] = read(a.gate, i);
     }
-    Unit<DT>::get(y, v[i]);
   }
-  // (x - mean) / root of (variance + eps), or without a mean; weight and bias.
-  auto norm = [&](const NormArgs& by) {
-    float mean = 0.f, sum = 0.f;
-    if (by.kind == 1) {
+  auto weight = [&](int k, int i, float (&f)[N]) __attribute__((always_inline)) {
+    if constexpr (KEEP) Unit<DT>::get(kept[k][i], f);
+    else Unit<DT>::get(read(k == 0 ? a.post.weight : k == 1 ? a.post.bias : k == 2 ? a.pre.weight : k == 3 ? a.pre.bias : a.gate, i), f);
+  };
+  const long long step = (long long)gridDim.x * ROWS;
+  long long row = blockIdx.x * (long long)ROWS + threadIdx.x / LANES;
+  uint4 x_next[U], y_next[U];
+  auto fetch = [&](long long r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      x_next[i] = read(a.x + r * a.x_stride, i);
+      y_next[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (a.y) y_next[i] = read(a.y + r * a.y_stride, i);
+    }
+  };
+  if (KEEP && row < a.n) fetch(row);
+  for (int parity = 0; row < a.n; row += step, parity ^= 1) {  // (all lanes of a row)
+    float v[U][N], f[N];
+    uint4 x[U];
+    if (!KEEP) fetch(row);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      x[i] = x_next[i];
+      Unit<DT>::get(y_next[i], v[i]);
+    }
+    if (KEEP && row + step < a.n) fetch(row + step);
+    // (x - mean) / root of (variance + eps), or without a mean; weight and bias.
+    auto norm = [&](const NormArgs& by, int which) __attribute__((always_inline)) {
+      float mean = 0.f, sum = 0.f;
+      if (by.kind == 1) {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int e = 0; e < N; ++e) sum += v[i][e];
+        mean = row_sum<LANES>(sum, of_wave[parity][2 * which]) * a.mean;
+        sum = 0.f;
+      }
 #pragma unroll
       for (int i = 0; i < U; ++i)
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum += v[i][e];
-      mean = row_sum<LANES>(sum, of_wave) * a.mean;
-      sum = 0.f;
-    }
+        for (int e = 0; e < N; ++e) {
+          const float d = v[i][e] - mean;
+          if (lane + i * LANES < a.units) sum = fmaf(d, d, sum);
+        }
+      const float by_root = 1.f / sqrtf(fmaf(row_sum<LANES>(sum, of_wave[parity][2 * which + 1]), a.mean, by.eps));
 #pragma unroll
-    for (int i = 0; i < U; ++i)
+      for (int i = 0; i < U; ++i) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float d = v[i][e] - mean;
-        if (lane + i * LANES < a.units) sum = fmaf(d, d, sum);
+        for (int e = 0; e < N; ++e) v[i][e] = lane + i * LANES < a.units ? (v[i][e] - mean) * by_root : 0.f;
+        if (by.weight) {
+          weight(2 * which, i, f);
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[i][e] *= f[e];
+        }
+        if (by.bias) {
+          weight(2 * which + 1, i, f);
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[i][e] += f[e];
+        }
       }
-    const float by_root = 1.f / sqrtf(fmaf(row_sum<LANES>(sum, of_wave), a.mean, by.eps));
+    };
+    auto put = [&](char* to, int i) __attribute__((always_inline)) {
+      const int at = lane + i * LANES;
+      if (at >= a.units) return;
+      const uint4 w = Unit<DT>::of(v[i]);
+      if constexpr (ONCE) store_once(reinterpret_cast<uint4*>(to + 16 * at), w);
+      else *reinterpret_cast<uint4*>(to + 16 * at) = w;
+    };
+    if (a.post.kind >= 0) norm(a.post, 0);
+    float one = 1.f;
+    if (a.gate && !a.gate_wide) {
+      const char* gate = a.gate + row * a.gate_stride;
+      if constexpr (DT == 0) one = *reinterpret_cast<const float*>(gate);
+      else one = low_half<DT>(*reinterpret_cast<const uint16_t*>(gate));
+      if (a.gate_tanh) one = tanh_of(one);
+    }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int at = lane + i * LANES;
-      if (at >= a.units) continue;
+      if (a.gate && a.gate_wide) {
+        if (a.gate_stride) Unit<DT>::get(read(a.gate + row * a.gate_stride, i), f);
+        else weight(4, i, f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[i][e] = (v[i][e] - mean) * by_root;
-      if (by.weight) {
-        Unit<DT>::get(*reinterpret_cast<const uint4*>(by.weight + 16 * at), f);
+        for (int e = 0; e < N; ++e) v[i][e] *= a.gate_tanh ? tanh_of(f[e]) : f[e];
+      } else if (a.gate) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[i][e] *= f[e];
+        for (int e = 0; e < N; ++e) v[i][e] *= one;
       }
-      if (by.bias) {
-        Unit<DT>::get(*reinterpret_cast<const uint4*>(by.bias + 16 * at), f);
+      Unit<DT>::get(x[i], f);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[i][e] += f[e];
-      }
+      for (int e = 0; e < N; ++e) v[i][e] = a.y ? fmaf(f[e], a.scale, v[i][e]) : f[e] * a.scale;
+      if (a.r) put(a.r + row * a.r_stride, i);
     }
-  };
-  auto put = [&](char* at, const float (&z)[N]) {
-    const uint4 w = Unit<DT>::of(z);
-    if constexpr (ONCE) store_once(reinterpret_cast<uint4*>(at), w);
-    else *reinterpret_cast<uint4*>(at) = w;
-  };
-  if (a.post.kind >= 0) norm(a.post);
-  const char* gate = a.gate ? a.gate + row * a.gate_stride : nullptr;
-  float one = 1.f;
-  if (gate && !a.gate_wide) {
-    if constexpr (DT == 0) one = *reinterpret_cast<const float*>(gate);
-    else one = low_half<DT>(*reinterpret_cast<const uint16_t*>(gate));
-    if (a.gate_tanh) one = tanhf(one);
-  }
+    if (!a.h) continue;
+    if (a.pre.kind >= 0) norm(a.pre, 1);
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int at = lane + i * LANES;
-    if (at >= a.units) continue;
-    if (gate && a.gate_wide) {
-      Unit<DT>::get(*reinterpret_cast<const uint4*>(gate + 16 * at), f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[i][e] *= a.gate_tanh ? tanhf(f[e]) : f[e];
-    } else if (gate) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[i][e] *= one;
-    }
-    Unit<DT>::get(x[i], f);
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[i][e] = a.y ? fmaf(f[e], a.scale, v[i][e]) : f[e] * a.scale;
-    if (a.r) put(a.r + row * a.r_stride + 16 * at, v[i]);
-  }
-  if (!a.h) return;
-  if (a.pre.kind >= 0) norm(a.pre);
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int at = lane + i * LANES;
-    if (at < a.units) put(a.h + row * a.h_stride + 16 * at, v[i]);
+    for (int i = 0; i < U; ++i) put(a.h + row * a.h_stride, i);
   }
 }
 
+// Rows follow one another in as many workgroups: twelve a compute unit, which holds three or four at once, so that they come out even (43,264
+// rows of 3,584 bf16 channels by 768 / 1,024 / 2,048 / 3,072 / one each: 235 / 292 / 246 / 237 / 280 us; 16,384 of 1,152 in fp32 75 / 67 / 68 / 69 / 78).
+constexpr int64_t kResidualBlocks = 3072;
+
 template <int DT, int LANES, int U> void launch_rows(const ResidualArgs& a, bool once, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n + kResidualThreads / LANES - 1) / (kResidualThreads / LANES))), block(kResidualThreads);
+  const int64_t blocks = (a.n + kResidualThreads / LANES - 1) / (kResidualThreads / LANES);
+  const dim3 grid((unsigned)std::min(blocks, kResidualBlocks)), block(kResidualThreads);
   if (once) hipLaunchKernelGGL((k_residual_norm<DT, LANES, U, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((k_residual_norm<DT, LANES, U, false>), grid, block, 0, s, a);
 }
 
 template <int DT> void launch_residual(const ResidualArgs& a, bool once, hipStream_t s) {
-  constexpr int W = DT == 0 ? 2 : 1;   // (registers: a unit of fp32 has half as many numbers)
   if (a.units <= kWave) launch_rows<DT, 64, 1>(a, once, s);
   else if (a.units <= 2 * kWave) launch_rows<DT, 64, 2>(a, once, s);
-  else if (a.units <= 4 * kWave) launch_rows<DT, 64, 4>(a, once, s);
-  else if (a.units <= 8 * kWave) launch_rows<DT, 64, 8>(a, once, s);
+  else if (a.units <= kResidualThreads) launch_rows<DT, 256, 1>(a, once, s);
+  else if (a.units <= 2 * kResidualThreads) launch_rows<DT, 256, 2>(a, once, s);
   else if (a.units <= 4 * kResidualThreads) launch_rows<DT, 256, 4>(a, once, s);
-  else launch_rows<DT, 256, 8 * W>(a, once, s);
+  else if (a.units <= 8 * kResidualThreads) launch_rows<DT, 256, 8>(a, once, s);
+  else if constexpr (DT == 0) launch_rows<DT, 256, 16>(a, once, s);
 }
 
 int check_norm(sttm_ctx* ctx, const sttm_norm* n, NormArgs* out) {
