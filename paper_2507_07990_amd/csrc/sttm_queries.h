@@ -29,6 +29,9 @@ struct QueryArgs {
   int parts, first_part;         // parts of a row in all, and where this launch's chunks begin among them
 };
 
+// Packed rows, pages, or pages of which token j of a segment's n sees the slots before length - (n - 1 - j).
+constexpr int kPacked = 0, kPaged = 1, kCausal = 2;
+
 // Where the segments' keys and values lie: in pages (table) or one segment after the other (offsets).
 struct KeyArgs {
   Pool pool;                     // packed rows: a page for each segment that begins at its first row
@@ -39,10 +42,10 @@ struct KeyArgs {
   long long rows;
   int max_len;
   long long token_stride;        // bytes
-  int from_each, slot_mask;      // pages: ~0, the slots of a page less one; packed: 0, all
+  int slot_mask;                 // the slots of a page less one
   const float* bias;             // NULL: none. Of slot i: bias[segment * bias_segment + h * bias_head + i] (packed: + the first row)
   long long bias_segment, bias_head;
-  int causal;                    // token j of a segment's n sees the slots before length - (n - 1 - j)
+  int kind;
   int chunk, chunks;
 };
 

@@ -254,7 +254,7 @@ KeyArgs make_paged(const sttm_cache* c, const sttm_sequences* s, const float* bi
   k.table_stride = seqs.table_stride;
   k.max_len = seqs.max_len;
   k.token_stride = k.pool.token_stride;
-  k.from_each = ~0;
+  k.kind = kPaged;
   k.slot_mask = c->page_size - 1;
   k.bias = bias;
   k.bias_segment = c->kv_heads * slots;
@@ -301,7 +301,7 @@ extern "C" int sttm_cross_attention(sttm_ctx* ctx, const sttm_states* states, in
   k.rows = states->rows;
   k.max_len = (int)max_len;
   k.token_stride = states->row_stride * es;
-  k.slot_mask = 0x7fffffff;
+  k.kind = kPacked;
   k.bias = key_bias;
   k.bias_head = bias_stride;
   return launch(ctx, states->dtype, QueryArgs{}, KeyArgs{}, b, k, p, static_cast<char*>(workspace));
@@ -341,7 +341,7 @@ extern "C" int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, con
   const QueryArgs b = make_queries(cache->dtype, tokens, seqs->batch, q_heads, cache->kv_heads, cache->head_dim, scale, q, q_stride, q_offsets, out,
                                    out_stride, lse);
   KeyArgs kb = make_paged(cache, seqs, key_bias, key_slots), ka{};
-  kb.causal = 1;
+  kb.kind = kCausal;
   QueryArgs a = b;
   if (p.a.chunks) {
     a.cuts = group_offsets;

@@ -164,11 +164,12 @@ template <int DT, int DP, bool FEW> struct Shape {
 // P is rounded to 16 bits for 16-bit values (half a step of the type: as much as the rounding of the result, which the sum over keys
 // mostly averages away); the sum that divides is that of the unrounded ones, in 32 bits. In fp16 it is 2^15 P, so that a weight is
 // off by no more than 2^-40 of the largest one where fp16 runs out of exponents.
-template <int DT, int DP, bool FEW, bool CAUSAL, bool FULL>
+template <int DT, int DP, bool FEW, int KIND, bool FULL>
 __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_a_simd(DT, DP)) k_query_tiles(QueryArgs a, KeyArgs kk) {
   using S = Shape<DT, DP, FEW>;
   constexpr int ES = S::ES, ROW = S::ROW, CH = S::CH, NQ = S::NQ, M = S::M, SETS = S::SETS, BUFFERS = S::BUFFERS, NK = S::NK, KT = S::KT;
   constexpr int AT_ONCE = S::AT_ONCE, PER = S::PER, TILE = S::TILE;
+  constexpr bool PAGED = KIND != kPacked, CAUSAL = KIND == kCausal;
   constexpr float LIFT = DT == 2 ? 15.f : 0.f;
   constexpr float UNLIFT = DT == 2 ? 1.f / 32768.f : 1.f;
   constexpr int K_AHEAD = DT == 0 ? 2 : 4, V_AHEAD = 2;  // pieces of keys, steps of values read ahead
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   }
 
   const float* bias = kk.bias ? kk.bias + s * kk.bias_segment + h * kk.bias_head + key0 : nullptr;
-  const int32_t* table = kk.table ? kk.table + s * kk.table_stride : nullptr;
+  const int32_t* table = PAGED ? kk.table + s * kk.table_stride : nullptr;
   const long long base = h * kk.pool.head_stride + key0 * kk.token_stride;
   const int stride = (int)kk.token_stride;                // (a block's rows lie within 2 GiB)
 
@@ -232,36 +233,50 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   auto key_from = [&](int i) STTM_INLINE { return 16 * (lane % CH ^ key_order<CH>(brought + AT_ONCE * S::SHARE * i + own_row)); };
   auto value_from = [&](int i) STTM_INLINE { return 16 * (lane % CH ^ value_order<DT, CH>(brought + AT_ONCE * S::SHARE * i + own_row)); };
   // Lane i: the page of key i of the block that is loaded next and its bias, looked up a block ahead; of the block on its way, what is added to the
-  // key's score. Keys from the end on: the page of the last one, whose other slots may be read.
-  int page_next = 0, page_now = 0;                        // (packed: 0)
+  // key's score and where its row is. Keys from the end on: the page of the last one, whose other slots may be read.
+  int page_next = 0;
   float bias_next = 0.f, add_now = 0.f;
+  unsigned long long from_now = 0;                        // (packed: of the block's first row, the same in all lanes)
+  int last_now = 0;                                       // (packed: of the last row there is, as seen from the block's first, or further)
   auto look_up = [&](int s0) STTM_INLINE {
     const int slot = min(s0 + min(lane, NK - 1), end - 1);
-    if (table) page_next = table[slot >> kk.pool.shift];
+    if constexpr (PAGED) page_next = table[slot >> kk.pool.shift];
     if (bias) bias_next = bias[slot];
   };
+  const char *const k_base = kk.pool.k + base, *const v_base = kk.pool.v + base;
   auto next_block = [&](int s0) STTM_INLINE {
-    const bool there = !table || (unsigned)page_next < (unsigned)kk.pool.pages;
+    const bool there = !PAGED || (unsigned)page_next < (unsigned)kk.pool.pages;
     add_now = lane >= NK || s0 + lane >= end || !there ? -INFINITY : bias_next;
-    page_now = there ? page_next : 0;                     // (what is read of a page that is not there does not count)
-  };
-  // (As many loads whatever the width and the source, one after the other, for the sake of those that count them: pieces behind a head's channels
-  // come from a place of zeros. Pages: each load from the start of its rows. Packed: from the block's first row, rows from the end on the last one.)
-  const int each = kk.from_each, slot_mask = kk.slot_mask;
-  const unsigned long long page_stride = kk.pool.page_stride;
-  const int own_from = own_row * stride;
-  auto load = [&](auto what, int s0, char* keys_to, char* values_to) STTM_INLINE {
-    constexpr bool KEYS = decltype(what)::value & 1, VALUES = decltype(what)::value & 2;
-    const int at_lds = (set * NK + brought) * ROW, last = kk.table ? 0x7fffffff : min(end - 1 - s0, NK) * stride;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int r = brought + AT_ONCE * S::SHARE * i, at = at_lds + AT_ONCE * S::SHARE * i * ROW;
-      const long long from = base + (unsigned)__builtin_amdgcn_readlane(page_now, r) * page_stride + (unsigned long long)(unsigned)((s0 + (r & each)) & slot_mask) * (unsigned)stride;
-      const unsigned row = (unsigned)min(own_from + (r & ~each) * stride, last);
-      const char *k_from = kk.pool.k + from, *v_from = kk.pool.v + from;
-      if constexpr (KEYS) to_lds(FULL || key_from(i) < kk.pool.row ? k_from + (row + key_from(i)) : kZeros, keys_to + at);
-      if constexpr (VALUES) to_lds(FULL || value_from(i) < kk.pool.row ? v_from + (row + value_from(i)) : kZeros, values_to + at);
+    if constexpr (PAGED) {                                // (what is read of a page that is not there does not count)
+      const int slot = min(s0 + min(lane, NK - 1), end - 1) & kk.slot_mask;
+      from_now = (unsigned long long)(unsigned)(there ? page_next : 0) * (unsigned long long)kk.pool.page_stride + (unsigned long long)(unsigned)slot * (unsigned)stride;
+    } else {
+      from_now = (unsigned long long)(unsigned)s0 * (unsigned long long)kk.token_stride;
+      last_now = min(end - 1 - s0, NK) * stride;
     }
+  };
+  // Load i of a block's keys, values. As many loads whatever the width, for the sake of those that count them: pieces behind a head's channels come
+  // from a place of zeros. Pages: from the start of the load's rows, which lie in one page. Packed: from the block's first row, rows from the end on
+  // the last one.
+  const int own_from = own_row * stride;
+  auto load_one = [&](auto what, int i, char* keys_to, char* values_to) STTM_INLINE {
+    constexpr bool KEYS = decltype(what)::value & 1, VALUES = decltype(what)::value & 2;
+    const int r = brought + AT_ONCE * S::SHARE * i, at = (set * NK + r) * ROW;
+    unsigned long long from = from_now;
+    unsigned row = own_from;
+    if constexpr (PAGED) {
+      from = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)from_now, r) |
+             (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(from_now >> 32), r) << 32;
+    } else {
+      row = (unsigned)min(own_from + r * stride, last_now);
+    }
+    const char *k_from = k_base + from, *v_from = v_base + from;
+    if constexpr (KEYS) to_lds(FULL || key_from(i) < kk.pool.row ? k_from + (row + key_from(i)) : kZeros, keys_to + at);
+    if constexpr (VALUES) to_lds(FULL || value_from(i) < kk.pool.row ? v_from + (row + value_from(i)) : kZeros, values_to + at);
+  };
+  auto load = [&](auto what, char* keys_to, char* values_to) STTM_INLINE {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) load_one(what, i, keys_to, values_to);
   };
   using Keys = std::integral_constant<int, 1>;
   using Values = std::integral_constant<int, 2>;
@@ -292,10 +307,10 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   if (start < end) {
     look_up(start);
     next_block(start);
-    if constexpr (FEW) load(Keys(), start, keys0, values0);
-    else load(Both(), start, keys0, values0);
+    if constexpr (FEW) load(Keys(), keys0, values0);
+    else load(Both(), keys0, values0);
     look_up(start + step);
-    if constexpr (FEW) load(Values(), start, keys0, values0);
+    if constexpr (FEW) load(Values(), keys0, values0);
   }
   arrived<0>();                                           // (the queries, too, which the compiler would wait for with every block else)
   // A block's keys (values) that count for none of the rows, or values that are not finite where not all rows see them: nothing of those may be
@@ -323,7 +338,8 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   };
   // One block. FEW: a wavefront has its block to itself, one buffer for keys and one for values; the next keys are on their way from the first
   // product on, the next values from the second.
-  auto block = [&](int s0, bool more, bool diagonal, bool whole, unsigned long long alive, const char* keys, char* values, const float* added) STTM_INLINE {
+  auto block = [&](int s0, bool more, bool diagonal, bool whole, unsigned long long alive, const char* keys, char* values, const float* added,
+                   char* next_keys, char* next_values) STTM_INLINE {
     // S^T. The pieces of keys are read a few products ahead (a read takes as long as four of them).
     f32x16 x[KT];
 #pragma unroll
@@ -352,6 +368,11 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       }
       __builtin_amdgcn_sched_barrier(0);
       if (c + K_AHEAD < NQ) read_keys(c + K_AHEAD);
+      if constexpr (!FEW) {                               // (the next block's loads while products go on)
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i * NQ / PER == c) load_one(Both(), i, next_keys, next_values);
+      }
     }
     // Values, the first ones on their way while the softmax goes on: of step j the keys that one product takes (16, fp32: 1 a half).
     constexpr int STEPS = DT == 0 ? 16 * KT : NK / 16;
@@ -373,7 +394,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       __builtin_amdgcn_wave_barrier();
       if (more) {
         next_block(s0 + step);
-        load(Keys(), s0 + step, keys0, values0);
+        load(Keys(), keys0, values0);
       }
     } else {
       read_values(0);
@@ -486,19 +507,17 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       __builtin_amdgcn_wave_barrier();
     } else {
       __syncthreads();
-      if (more) {
-        next_block(s0 + step);
-        load(Both(), s0 + step, next_keys, next_values);
-        look_up(s0 + 2 * step);
-      }
+      next_block(more ? s0 + step : s0);                  // (behind the last block comes that one again: no way of its own for it)
     }
-    block(s0, more, diagonal, whole, alive, keys, values, added);
-    if constexpr (FEW) {
+    block(s0, more, diagonal, whole, alive, keys, values, added, next_keys, next_values);
+    if constexpr (!FEW) {
+      look_up(s0 + 2 * step);
+    } else {
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_wave_barrier();
       if (more) {
         look_up(s0 + 2 * step);
-        load(Values(), s0 + step, keys0, values0);
+        load(Values(), keys0, values0);
       }
     }
   };
@@ -510,6 +529,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       if (s0 + step < end) one(s0 + step, keys1, values1, keys0, values0, adds[0][BUFFERS - 1]);
     }
   }
+  arrived<0>();                                           // (nothing may come into LDS any more)
   settle();
 
   const bool parted = a.part && !(a.alone && length <= kk.chunk);
@@ -584,9 +604,9 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       float add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
       for (int i = max(first, least - NK + 1); i < min(end, limit); ++i) {
-        const int page = table ? table[i >> kk.pool.shift] : 0;
-        if ((table && (unsigned)page >= (unsigned)kk.pool.pages) || (bias && bias[i] == -INFINITY)) continue;
-        const long long at = base + (table ? page * kk.pool.page_stride + (i & slot_mask) * stride : i * kk.token_stride);
+        const int page = PAGED ? table[i >> kk.pool.shift] : 0;
+        if ((PAGED && (unsigned)page >= (unsigned)kk.pool.pages) || (bias && bias[i] == -INFINITY)) continue;
+        const long long at = base + (PAGED ? page * kk.pool.page_stride + (i & kk.slot_mask) * stride : i * kk.token_stride);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float v;
@@ -608,17 +628,23 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   }
 }
 
-template <int DT, int DP, bool FEW, bool CAUSAL>
+template <int DT, int DP, bool FEW, int KIND>
 void launch_tiles(const QueryArgs& a, const KeyArgs& k, hipStream_t s) {
   const dim3 grid((unsigned)(a.tokens * a.group / query_tile(FEW) + a.segments), a.kv_heads, k.chunks), block(Shape<DT, DP, FEW>::THREADS);
-  if (k.pool.row == Shape<DT, DP, FEW>::ROW) hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, CAUSAL, true>), grid, block, 0, s, a, k);
-  else hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, CAUSAL, false>), grid, block, 0, s, a, k);
+  if (k.pool.row == Shape<DT, DP, FEW>::ROW) hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, KIND, true>), grid, block, 0, s, a, k);
+  else hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, KIND, false>), grid, block, 0, s, a, k);
+}
+
+template <int DT, int DP, bool FEW>
+void launch_kind(const QueryArgs& a, const KeyArgs& k, hipStream_t s) {
+  if (k.kind == kPacked) launch_tiles<DT, DP, FEW, kPacked>(a, k, s);
+  else if (k.kind == kPaged) launch_tiles<DT, DP, FEW, kPaged>(a, k, s);
+  else launch_tiles<DT, DP, FEW, kCausal>(a, k, s);
 }
 
 template <int DT, int DP>
 void launch_width(const QueryArgs& a, const KeyArgs& k, bool few, hipStream_t s) {
-  if (few) k.causal ? launch_tiles<DT, DP, true, true>(a, k, s) : launch_tiles<DT, DP, true, false>(a, k, s);
-  else k.causal ? launch_tiles<DT, DP, false, true>(a, k, s) : launch_tiles<DT, DP, false, false>(a, k, s);
+  few ? launch_kind<DT, DP, true>(a, k, s) : launch_kind<DT, DP, false>(a, k, s);
 }
 
 }  // namespace
