@@ -1,6 +1,6 @@
 // Attention of several queries: the rows of a segment's tokens over the segment's keys, in the packed rows of a batch or in the pages of a
-// cache. One kernel for all element types and head sizes; the entry points (sttm_queries.hip) launch it once for each kind of
-// segment and put parts together.
+// cache. One kernel for all element types and head sizes; the entry points (sttm_queries.hip) launch it once and put parts
+// together.
 #pragma once
 #include "sttm_cache.h"
 
@@ -25,12 +25,9 @@ struct QueryArgs {
   float scale;
   float* part;                   // [tokens, q_heads, parts, d]: unnormalised sums (more than one part), else NULL
   float2* stat;                  // [tokens, q_heads, parts]: largest score and sum of exponentials of a part
-  int alone;                     // no other launch has parts of these rows: a segment of one chunk has its result right away
-  int parts, first_part;         // parts of a row in all, and where this launch's chunks begin among them
+  int alone;                     // no other kind has parts of these rows: a segment of one chunk has its result right away
+  int parts, first_part;         // parts of a row in all, and where this kind's chunks begin among them
 };
-
-// Packed rows, pages, or pages of which token j of a segment's n sees the slots before length - (n - 1 - j).
-constexpr int kPacked = 0, kPaged = 1, kCausal = 2;
 
 // Where the segments' keys and values lie: in pages (table) or one segment after the other (offsets).
 struct KeyArgs {
@@ -45,8 +42,17 @@ struct KeyArgs {
   int slot_mask;                 // the slots of a page less one
   const float* bias;             // NULL: none. Of slot i: bias[segment * bias_segment + h * bias_head + i] (packed: + the first row)
   long long bias_segment, bias_head;
-  int kind;
+  int causal;                    // (pages) token j of a segment's n sees the slots before length - (n - 1 - j)
   int chunk, chunks;
+};
+
+// What one launch does: up to two kinds of segments, the workgroups of the first one in front.
+struct QueryJobs {
+  QueryArgs q[2];
+  KeyArgs k[2];
+  int count;
+  unsigned tiles[2];             // tiles of rows
+  unsigned first, all;           // workgroups of the first kind, of both
 };
 
 __device__ inline long long clamped(long long x, long long most) { return min(max(x, 0ll), most); }
@@ -88,9 +94,9 @@ __device__ inline int segment_length(const KeyArgs& k, int s, long long* first) 
 // lowest fp32 number, or near the largest, and has no multiple then.)
 __device__ inline float query_factor(float m, float top) { return exp2_fast((m - (top == -INFINITY ? 0.f : top)) * kLog2e); }
 
-// One launch of the kernel for one kind of segment. rows_of_wave: a workgroup has 32 rows, its four wavefronts take blocks of keys in
+// One launch of the kernel. few_rows: a workgroup has 32 rows, its four wavefronts take blocks of keys in
 // turn; else 128 rows that share the blocks.
-template <int DT> void launch_queries(const QueryArgs& a, const KeyArgs& k, bool few_rows, hipStream_t s);
+template <int DT> void launch_queries(QueryJobs& jobs, bool few_rows, hipStream_t s);
 // Rows of a workgroup's tile for this kind.
 inline int query_tile(bool few_rows) { return few_rows ? kRowTile : kRowTile * kQueryWaves; }
 // Bytes of a head's row in LDS: a power of two; above 512 a tile of its own for each wavefront would not fit.

@@ -29,7 +29,7 @@ __device__ inline int parts_of(const QueryArgs& a, const KeyArgs& k, int b) {
   return max((length + k.chunk - 1) / k.chunk, 1);
 }
 
-// A row's parts on a common maximum: those of the first launch, then those of the second, added up in a fixed order. Tokens of no sequence stay
+// A row's parts on a common maximum: those of the prefix, then its own, added up in a fixed order. Tokens of no sequence stay
 // as they are, and rows whose only part is their result already.
 // LANES lanes have a row, four channels each, the parts dealt out among as many groups of lanes as there are. A workgroup where there are few rows (their
 // parts come from all over memory at once: 32 tokens, 28 heads, 58 parts of 128 channels 9 us), a wavefront with four of a token's heads in turn else.
@@ -91,17 +91,16 @@ constexpr double kEnds = 3, kJoin = 2, kPart = 5e-7;
 
 // How the keys of one kind of segment are cut.
 struct Cut {
-  bool few;
   int chunk, chunks;
 };
-Cut make_cut(int64_t tokens, int group, int segments, int kv_heads, int64_t max_len, int d, int es) {
-  Cut c{false, 64, 1};
+bool few_rows(int64_t tokens, int group, int segments) { return tokens * group <= (int64_t)kRowTile * segments; }
+Cut make_cut(bool few, int64_t tokens, int group, int segments, int kv_heads, int64_t max_len, int d, int es) {
+  Cut c{64, 1};
   if (segments < 1) return c;
   const int64_t rows = tokens * group, row_bytes = query_row_bytes(d, es);
-  c.few = rows <= (int64_t)kRowTile * segments && row_bytes <= 1024;
   // Workgroups of one chunk each: at most one a tile more than the rows fill, and a compute unit holds two (few rows, wide rows: one).
-  const int64_t tiles = (rows / query_tile(c.few) + std::min<int64_t>(segments, rows)) * kv_heads, slots = row_bytes > 512 || (!c.few && row_bytes > 256) ? 256 : 512;
-  if (c.few) {
+  const int64_t tiles = (rows / query_tile(few) + std::min<int64_t>(segments, rows)) * kv_heads, slots = row_bytes > 512 || (!few && row_bytes > 256) ? 256 : 512;
+  if (few) {
     // Bound by memory and by how even the load is: chunks of 1,024 keys, shorter ones where those would not make three or four rounds (whole calls by
     // 256 / 512 / 1,024 / 2,048, us: 32 sequences of 1,013 to 8,117 keys, 64 heads on 8 of 128 bf16 channels 125 / 110 / 106 / 119; 5 of 333 to 4,979,
     // 16 heads of 72, fp32 85 / 91 / 109 / 204); one for short ones, where a second launch costs more than blocks that follow each other (257
@@ -109,6 +108,7 @@ Cut make_cut(int64_t tokens, int group, int segments, int kv_heads, int64_t max_
     c.chunk = 1024;
     while (c.chunk > 256 && tiles * ((max_len + c.chunk - 1) / c.chunk) < 1800) c.chunk /= 2;
     if (max_len <= 512) c.chunk = 512;
+    while ((int64_t)segments * ((max_len + c.chunk - 1) / c.chunk) > 1 << 20) c.chunk *= 2;      // (a grid has fewer than 2^32 workgroups)
     c.chunks = (int)std::max<int64_t>(1, (max_len + c.chunk - 1) / c.chunk);
     return c;
   }
@@ -132,12 +132,13 @@ Cut make_cut(int64_t tokens, int group, int segments, int kv_heads, int64_t max_
 }
 
 struct Plan {
+  bool few;
   Cut a, b;          // segments of several sequences (none: no chunks), segments of one
   int parts;
   size_t part, stat, bytes;
 };
-Plan make_plan(Cut a, Cut b, int64_t tokens, int q_heads, int d) {
-  Plan p{a, b, a.chunks + b.chunks, 0, 0, 0};
+Plan make_plan(bool few, Cut a, Cut b, int64_t tokens, int q_heads, int d) {
+  Plan p{few, a, b, a.chunks + b.chunks, 0, 0, 0};
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
   const size_t rows = p.parts > 1 ? (size_t)tokens * q_heads * p.parts : 0;
@@ -187,20 +188,31 @@ int check_rows(sttm_ctx* ctx, int dtype, int head_dim, int q_heads, int64_t toke
 }
 
 Plan plan_cross(const sttm_states* s, int64_t tokens, int q_heads) {
-  const Cut b = make_cut(tokens, q_heads / s->kv_heads, s->batch, s->kv_heads, std::min<int64_t>(s->max_rows, s->rows), s->head_dim, elem_bytes(s->dtype));
-  return make_plan(Cut{false, 1, 0}, b, tokens, q_heads, s->head_dim);
+  const int group = q_heads / s->kv_heads;
+  const bool few = few_rows(tokens, group, s->batch);
+  const Cut b = make_cut(few, tokens, group, s->batch, s->kv_heads, std::min<int64_t>(s->max_rows, s->rows), s->head_dim, elem_bytes(s->dtype));
+  return make_plan(few, Cut{1, 0}, b, tokens, q_heads, s->head_dim);
 }
 
+// (Prefixes and own slots in one launch, with tiles of one size: those of the prefixes, whose rows are more.)
 Plan plan_shared(const sttm_cache* c, const sttm_sequences* prefixes, const sttm_sequences* seqs, int64_t tokens, int q_heads) {
-  const int group = q_heads / c->kv_heads, es = elem_bytes(c->dtype);
-  Cut a{false, 1, 0};
-  if (prefixes && prefixes->batch) a = make_cut(tokens, group, prefixes->batch, c->kv_heads, make_seqs(c, prefixes).max_len, c->head_dim, es);
-  return make_plan(a, make_cut(tokens, group, seqs->batch, c->kv_heads, make_seqs(c, seqs).max_len, c->head_dim, es), tokens, q_heads, c->head_dim);
+  const int group = q_heads / c->kv_heads, es = elem_bytes(c->dtype), groups = prefixes ? prefixes->batch : 0;
+  const bool few = few_rows(tokens, group, groups ? groups : seqs->batch) && few_rows(tokens, group, seqs->batch);
+  Cut a{1, 0};
+  if (groups) a = make_cut(few, tokens, group, groups, c->kv_heads, make_seqs(c, prefixes).max_len, c->head_dim, es);
+  return make_plan(few, a, make_cut(few, tokens, group, seqs->batch, c->kv_heads, make_seqs(c, seqs).max_len, c->head_dim, es), tokens, q_heads, c->head_dim);
 }
 
 template <int DT> void launch_all(QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb, const Plan& p, hipStream_t s) {
-  if (p.a.chunks) launch_queries<DT>(a, ka, p.a.few, s);
-  launch_queries<DT>(b, kb, p.b.few, s);
+  QueryJobs jobs{};
+  if (p.a.chunks) {
+    jobs.q[0] = a;
+    jobs.k[0] = ka;
+    jobs.count = 1;
+  }
+  jobs.q[jobs.count] = b;
+  jobs.k[jobs.count++] = kb;
+  launch_queries<DT>(jobs, p.few, s);
   if (p.parts < 2) return;
   const unsigned tokens = (unsigned)b.tokens, heads = b.kv_heads * b.group, some = kJoinHeads * (kJoinThreads / kWave);
   if ((int64_t)tokens * heads < kJoinWaves) hipLaunchKernelGGL((k_query_join<DT, kJoinThreads>), dim3(tokens, heads), dim3(kJoinThreads), 0, s, a, ka, b, kb);
@@ -254,7 +266,6 @@ KeyArgs make_paged(const sttm_cache* c, const sttm_sequences* s, const float* bi
   k.table_stride = seqs.table_stride;
   k.max_len = seqs.max_len;
   k.token_stride = k.pool.token_stride;
-  k.kind = kPaged;
   k.slot_mask = c->page_size - 1;
   k.bias = bias;
   k.bias_segment = c->kv_heads * slots;
@@ -301,7 +312,6 @@ extern "C" int sttm_cross_attention(sttm_ctx* ctx, const sttm_states* states, in
   k.rows = states->rows;
   k.max_len = (int)max_len;
   k.token_stride = states->row_stride * es;
-  k.kind = kPacked;
   k.bias = key_bias;
   k.bias_head = bias_stride;
   return launch(ctx, states->dtype, QueryArgs{}, KeyArgs{}, b, k, p, static_cast<char*>(workspace));
@@ -341,7 +351,7 @@ extern "C" int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, con
   const QueryArgs b = make_queries(cache->dtype, tokens, seqs->batch, q_heads, cache->kv_heads, cache->head_dim, scale, q, q_stride, q_offsets, out,
                                    out_stride, lse);
   KeyArgs kb = make_paged(cache, seqs, key_bias, key_slots), ka{};
-  kb.kind = kCausal;
+  kb.causal = 1;
   QueryArgs a = b;
   if (p.a.chunks) {
     a.cuts = group_offsets;

@@ -1,3 +1,3 @@
 #include "sttm_queries_kernel.h"
 
-template void sttm::launch_queries<1>(const sttm::QueryArgs&, const sttm::KeyArgs&, bool, hipStream_t);  // bf16
+template void sttm::launch_queries<1>(sttm::QueryJobs&, bool, hipStream_t);  // bf16

@@ -1,3 +1,3 @@
 #include "sttm_queries_kernel.h"
 
-template void sttm::launch_queries<2>(const sttm::QueryArgs&, const sttm::KeyArgs&, bool, hipStream_t);  // f16
+template void sttm::launch_queries<2>(sttm::QueryJobs&, bool, hipStream_t);  // f16

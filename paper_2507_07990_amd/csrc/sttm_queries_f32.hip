@@ -1,3 +1,3 @@
 #include "sttm_queries_kernel.h"
 
-template void sttm::launch_queries<0>(const sttm::QueryArgs&, const sttm::KeyArgs&, bool, hipStream_t);  // f32
+template void sttm::launch_queries<0>(sttm::QueryJobs&, bool, hipStream_t);  // f32

@@ -153,6 +153,23 @@ template <int DT, int DP, bool FEW> struct Shape {
   static constexpr int TILE = kRowTile * SHARE;
 };
 
+// Which of n pieces of work, tiles fastest, workgroup id takes. Workgroups go to the eight dies in turn, and each die has an L2 of its own: the tiles of one
+// head and chunk, which read the same keys, go to one die; what is left over of eight of these, in eight runs (whole calls, us, against tiles in turn:
+// one prompt on 43,264 keys 275 against 302, ragged prompts 164 / 195, 32 answers behind 14,672 slots 60 / 65). Few rows share no keys.
+template <bool FEW> __device__ inline unsigned in_dies(unsigned id, unsigned n, unsigned tiles) {
+  constexpr unsigned DIES = 8;
+  if (FEW) return id;
+  const unsigned whole = n / (DIES * tiles) * (DIES * tiles);
+  unsigned run = tiles, begin = 0;
+  if (id >= whole) {
+    begin = whole;
+    run = (n - whole) / DIES;
+    if (id >= begin + run * DIES) return id;
+  }
+  const unsigned turn = (id - begin) / DIES, round = turn / run;
+  return begin + (round * DIES + (id - begin) % DIES) * run + (turn - round * run);
+}
+
 // One workgroup: a tile of rows (a token and a head of the kv head's group each) of one segment, one chunk of the segment's keys. FEW: 32
 // rows, the four wavefronts take blocks of 32 keys in turn, each with its own running maximum and sum, joined in LDS at the
 // end. Else 128 rows, 32 a wavefront, that share blocks of NK keys.
@@ -164,12 +181,12 @@ template <int DT, int DP, bool FEW> struct Shape {
 // P is rounded to 16 bits for 16-bit values (half a step of the type: as much as the rounding of the result, which the sum over keys
 // mostly averages away); the sum that divides is that of the unrounded ones, in 32 bits. In fp16 it is 2^15 P, so that a weight is
 // off by no more than 2^-40 of the largest one where fp16 runs out of exponents.
-template <int DT, int DP, bool FEW, int KIND, bool FULL>
-__global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_a_simd(DT, DP)) k_query_tiles(QueryArgs a, KeyArgs kk) {
+template <int DT, int DP, bool FEW, bool PAGED, bool FULL>
+__global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_a_simd(DT, DP)) k_query_tiles(QueryJobs jobs) {
   using S = Shape<DT, DP, FEW>;
   constexpr int ES = S::ES, ROW = S::ROW, CH = S::CH, NQ = S::NQ, M = S::M, SETS = S::SETS, BUFFERS = S::BUFFERS, NK = S::NK, KT = S::KT;
   constexpr int AT_ONCE = S::AT_ONCE, PER = S::PER, TILE = S::TILE;
-  constexpr bool PAGED = KIND != kPacked, CAUSAL = KIND == kCausal;
+  constexpr bool CAUSAL = PAGED;                          // (or may be)
   constexpr float LIFT = DT == 2 ? 15.f : 0.f;
   constexpr float UNLIFT = DT == 2 ? 1.f / 32768.f : 1.f;
   constexpr int K_AHEAD = DT == 0 ? 2 : 4, V_AHEAD = 2;  // pieces of keys, steps of values read ahead
@@ -184,7 +201,14 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   __shared__ int odd_value;                               // a value that is not finite in a block whose keys not all rows see
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, g = lane >> 5;
-  const int tile = blockIdx.x, h = blockIdx.y, chunk = blockIdx.z;
+  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x;
+  if (id >= jobs.all) return;
+  const unsigned which = PAGED && id >= jobs.first;
+  const QueryArgs& a = jobs.q[which];
+  const KeyArgs& kk = jobs.k[which];
+  const unsigned tiles = jobs.tiles[which], at = in_dies<FEW>(id - (which ? jobs.first : 0u), (which ? jobs.all - jobs.first : jobs.first), tiles);
+  const unsigned in_heads = at / tiles;
+  const int chunk = (int)(in_heads / (unsigned)a.kv_heads), h = (int)(in_heads - (unsigned)chunk * a.kv_heads), tile = (int)(at - in_heads * tiles);
   // Segment s has the tiles from first_token * group / TILE + s on: no two share one, and each has as many as it needs.
   const int s = last_not_above(a.segments, tile, [&](int i) { return first_token_of_segment(a, i) * a.group / TILE + i; });
   const long long token0 = first_token_of_segment(a, s);
@@ -203,7 +227,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   const long long in_row = min(row, rows - 1), in_token = in_row / a.group, token = token0 + in_token;
   const int head = h * a.group + (int)(in_row - in_token * a.group);
   int limit = length, end = min(length, first + kk.chunk), least = length;   // slots that the row, any row of the tile, all of them see
-  if constexpr (CAUSAL) {
+  if (CAUSAL && kk.causal) {
     const long long behind = length - rows / a.group + 1;
     limit = (int)max(behind + in_token, 0ll);
     least = (int)max(behind + row0 / a.group, 0ll);
@@ -628,33 +652,38 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   }
 }
 
-template <int DT, int DP, bool FEW, int KIND>
-void launch_tiles(const QueryArgs& a, const KeyArgs& k, hipStream_t s) {
-  const dim3 grid((unsigned)(a.tokens * a.group / query_tile(FEW) + a.segments), a.kv_heads, k.chunks), block(Shape<DT, DP, FEW>::THREADS);
-  if (k.pool.row == Shape<DT, DP, FEW>::ROW) hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, KIND, true>), grid, block, 0, s, a, k);
-  else hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, KIND, false>), grid, block, 0, s, a, k);
-}
-
-template <int DT, int DP, bool FEW>
-void launch_kind(const QueryArgs& a, const KeyArgs& k, hipStream_t s) {
-  if (k.kind == kPacked) launch_tiles<DT, DP, FEW, kPacked>(a, k, s);
-  else if (k.kind == kPaged) launch_tiles<DT, DP, FEW, kPaged>(a, k, s);
-  else launch_tiles<DT, DP, FEW, kCausal>(a, k, s);
+template <int DT, int DP, bool FEW, bool PAGED>
+void launch_tiles(const QueryJobs& jobs, hipStream_t s) {
+  const unsigned wide = std::min(jobs.all, 1u << 20);     // (fewer than 2^32 threads along a side of the grid)
+  const dim3 grid(wide, (jobs.all + wide - 1) / wide), block(Shape<DT, DP, FEW>::THREADS);
+  if (jobs.k[0].pool.row == Shape<DT, DP, FEW>::ROW) hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, PAGED, true>), grid, block, 0, s, jobs);
+  else hipLaunchKernelGGL((k_query_tiles<DT, DP, FEW, PAGED, false>), grid, block, 0, s, jobs);
 }
 
 template <int DT, int DP>
-void launch_width(const QueryArgs& a, const KeyArgs& k, bool few, hipStream_t s) {
-  few ? launch_kind<DT, DP, true>(a, k, s) : launch_kind<DT, DP, false>(a, k, s);
+void launch_width(const QueryJobs& jobs, bool few, hipStream_t s) {
+  const bool paged = !jobs.k[0].offsets;
+  if (few) paged ? launch_tiles<DT, DP, true, true>(jobs, s) : launch_tiles<DT, DP, true, false>(jobs, s);
+  else paged ? launch_tiles<DT, DP, false, true>(jobs, s) : launch_tiles<DT, DP, false, false>(jobs, s);
 }
 
 }  // namespace
 
-template <int DT> void launch_queries(const QueryArgs& a, const KeyArgs& k, bool few_rows, hipStream_t s) {
-  if (a.d <= 64) launch_width<DT, 64>(a, k, few_rows, s);
-  else if (a.d <= 96) launch_width<DT, 96>(a, k, few_rows, s);
-  else if (a.d <= 128) launch_width<DT, 128>(a, k, few_rows, s);
-  else if (a.d <= 192) launch_width<DT, 192>(a, k, few_rows, s);
-  else launch_width<DT, 256>(a, k, few_rows, s);
+template <int DT> void launch_queries(QueryJobs& jobs, bool few_rows, hipStream_t s) {
+  jobs.all = 0;
+  for (int i = 0; i < jobs.count; ++i) {
+    const QueryArgs& a = jobs.q[i];
+    jobs.tiles[i] = (unsigned)(a.tokens * a.group / query_tile(few_rows) + a.segments);
+    jobs.first = jobs.all;
+    jobs.all += jobs.tiles[i] * a.kv_heads * jobs.k[i].chunks;
+  }
+  if (jobs.count == 1) jobs.first = jobs.all;
+  const int d = jobs.q[0].d;
+  if (d <= 64) launch_width<DT, 64>(jobs, few_rows, s);
+  else if (d <= 96) launch_width<DT, 96>(jobs, few_rows, s);
+  else if (d <= 128) launch_width<DT, 128>(jobs, few_rows, s);
+  else if (d <= 192) launch_width<DT, 192>(jobs, few_rows, s);
+  else launch_width<DT, 256>(jobs, few_rows, s);
 }
 
 }  // namespace sttm
