@@ -86,8 +86,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_query_join(QueryArgs a, KeyArg
 
 // ---- launches -----------------------------------------------------------------------------------------------------
 
-// In blocks of 64 keys (2 us): a workgroup's beginning and end, a second launch, a channel of a part written and read again.
-constexpr double kEnds = 3, kJoin = 2, kPart = 5e-7;
+// In blocks of 64 keys (2 us): a workgroup's beginning and end, of the last one's time, a second launch, a channel of a part written and read again.
+constexpr double kEnds = 3, kTail = 0.75, kJoin = 2, kPart = 7e-7;
 
 // How the keys of one kind of segment are cut.
 struct Cut {
@@ -113,14 +113,17 @@ Cut make_cut(bool few, int64_t tokens, int group, int segments, int kv_heads, in
     return c;
   }
   // The cut with the least time, in units of a block of 64 keys: workgroups in rounds (one length), or all their work dealt out and the longest one
-  // behind it (lengths of half the largest on average), each with a beginning and an end; a second launch, and what it takes for each part of a row.
+  // behind it (lengths of half the largest on average), which has a compute unit to itself by then, each with a beginning and an end; a second launch, and what
+  // it takes to write and read each part of a row. Whole calls with chunks of 1,024 / 2,048 / 4,096 keys / one chunk, us: one prompt of 331 tokens on
+  // 43,264 keys, 28 heads on 4, 326 / 308 / 284 / 1,015 (the rule: 3,328, 272); ten of 19 to 160 on up to 6,491, 64 on 8, 181 / 165 / 165 / 158; eight of
+  // 13 to 211 behind two of up to 8,191 slots, 28 on 4, 126 / 111 / 179 / 252 (1,536: 140); 32 of one behind 43,264 slots 67 / 81 / 138 / 1,284 (the rule: 704, 60).
   const int64_t blocks = (max_len + 63) / 64;
   double best = 0;
   for (int64_t n = 1; n <= std::min<int64_t>(blocks, 256); ++n) {
     const int64_t chunk = (blocks + n - 1) / n;
     if ((blocks + chunk - 1) / chunk != n) continue;      // (as many blocks each as with fewer)
     const double work = (double)tiles * n * (chunk + kEnds) / slots;
-    const double time = segments == 1 ? std::ceil((double)tiles * n / slots) * (chunk + kEnds) : work / 2 + chunk + kEnds;
+    const double time = segments == 1 ? std::ceil((double)tiles * n / slots) * (chunk + kEnds) : work / 2 + (chunk + kEnds) * kTail;
     const double cost = time + (n > 1 ? kJoin + (double)rows * kv_heads * n * d * kPart : 0);
     if (n == 1 || cost < best) {
       best = cost;

@@ -153,6 +153,14 @@ template <int DT, int DP, bool FEW> struct Shape {
   static constexpr int TILE = kRowTile * SHARE;
 };
 
+// Held in a register, the same in all lanes: the compiler would read an argument anew in every block, and wait for it.
+template <class T> __device__ inline T held(T x) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm("" : "+s"(x));
+#endif
+  return x;
+}
+
 // Which of n pieces of work, tiles fastest, workgroup id takes. Workgroups go to the eight dies in turn, and each die has an L2 of its own: the tiles of one
 // head and chunk, which read the same keys, go to one die; what is left over of eight of these, in eight runs (whole calls, us, against tiles in turn:
 // one prompt on 43,264 keys 275 against 302, ragged prompts 164 / 195, 32 answers behind 14,672 slots 60 / 65). Few rows share no keys.
@@ -249,7 +257,10 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   const float* bias = kk.bias ? kk.bias + s * kk.bias_segment + h * kk.bias_head + key0 : nullptr;
   const int32_t* table = PAGED ? kk.table + s * kk.table_stride : nullptr;
   const long long base = h * kk.pool.head_stride + key0 * kk.token_stride;
-  const int stride = (int)kk.token_stride;                // (a block's rows lie within 2 GiB)
+  const int stride = (int)held(kk.token_stride);          // (a block's rows lie within 2 GiB)
+  const float scale = held(a.scale);
+  const int page_shift = held(kk.pool.shift), pages = held(kk.pool.pages), slot_mask = held(kk.slot_mask);
+  const long long page_stride = held(kk.pool.page_stride);
 
   // The pieces of LDS that this lane fills with load i: of row brought + AT_ONCE * SHARE * i (+ its own row of the AT_ONCE of a load), which lie
   // in one page. Pieces behind a head's channels stay zero.
@@ -264,16 +275,16 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   int last_now = 0;                                       // (packed: of the last row there is, as seen from the block's first, or further)
   auto look_up = [&](int s0) STTM_INLINE {
     const int slot = min(s0 + min(lane, NK - 1), end - 1);
-    if constexpr (PAGED) page_next = table[slot >> kk.pool.shift];
+    if constexpr (PAGED) page_next = table[slot >> page_shift];
     if (bias) bias_next = bias[slot];
   };
   const char *const k_base = kk.pool.k + base, *const v_base = kk.pool.v + base;
   auto next_block = [&](int s0) STTM_INLINE {
-    const bool there = !PAGED || (unsigned)page_next < (unsigned)kk.pool.pages;
+    const bool there = !PAGED || (unsigned)page_next < (unsigned)pages;
     add_now = lane >= NK || s0 + lane >= end || !there ? -INFINITY : bias_next;
     if constexpr (PAGED) {                                // (what is read of a page that is not there does not count)
-      const int slot = min(s0 + min(lane, NK - 1), end - 1) & kk.slot_mask;
-      from_now = (unsigned long long)(unsigned)(there ? page_next : 0) * (unsigned long long)kk.pool.page_stride + (unsigned long long)(unsigned)slot * (unsigned)stride;
+      const int slot = min(s0 + min(lane, NK - 1), end - 1) & slot_mask;
+      from_now = (unsigned long long)(unsigned)(there ? page_next : 0) * (unsigned long long)page_stride + (unsigned long long)(unsigned)slot * (unsigned)stride;
     } else {
       from_now = (unsigned long long)(unsigned)s0 * (unsigned long long)kk.token_stride;
       last_now = min(end - 1 - s0, NK) * stride;
@@ -364,40 +375,6 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   // product on, the next values from the second.
   auto block = [&](int s0, bool more, bool diagonal, bool whole, unsigned long long alive, const char* keys, char* values, const float* added,
                    char* next_keys, char* next_values) STTM_INLINE {
-    // S^T. The pieces of keys are read a few products ahead (a read takes as long as four of them).
-    f32x16 x[KT];
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[t][r] = 0.f;
-    w4 k[K_AHEAD][KT];
-    auto read_keys = [&](int c) STTM_INLINE {
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
-        k[c % K_AHEAD][t] = *reinterpret_cast<const w4*>(keys + key_at[c % NK_AT] + (32 * t * ROW + c / NK_AT * NK_AT * 32));
-    };
-#pragma unroll
-    for (int c = 0; c < K_AHEAD; ++c) read_keys(c);
-#pragma unroll
-    for (int c = 0; c < NQ; ++c) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        if constexpr (DT == 0) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[t] = mma32(__uint_as_float(k[c % K_AHEAD][t][e]), __uint_as_float(q[c][e]), x[t]);
-        } else {
-          x[t] = mma16<DT>(k[c % K_AHEAD][t], q[c], x[t]);
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (c + K_AHEAD < NQ) read_keys(c + K_AHEAD);
-      if constexpr (!FEW) {                               // (the next block's loads while products go on)
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (i * NQ / PER == c) load_one(Both(), i, next_keys, next_values);
-      }
-    }
     // Values, the first ones on their way while the softmax goes on: of step j the keys that one product takes (16, fp32: 1 a half).
     constexpr int STEPS = DT == 0 ? 16 * KT : NK / 16;
     w4 v[V_AHEAD][DT == 0 ? (M + 3) / 4 : M];
@@ -413,6 +390,50 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
         }
       }
     };
+    // S^T. The pieces of keys are read a few products ahead (a read takes as long as four of them).
+    f32x16 x[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[t][r] = 0.f;
+    w4 k[K_AHEAD][KT];
+    float4 add[KT * 4];
+    auto read_keys = [&](int c) STTM_INLINE {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+        k[c % K_AHEAD][t] = *reinterpret_cast<const w4*>(keys + key_at[c % NK_AT] + (32 * t * ROW + c / NK_AT * NK_AT * 32));
+    };
+#pragma unroll
+    for (int c = 0; c < K_AHEAD; ++c) read_keys(c);
+    if constexpr (!FEW) __builtin_amdgcn_s_setprio(1);    // (products first: the SIMD's other wavefront does its softmax behind them)
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        if constexpr (DT == 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[t] = mma32(__uint_as_float(k[c % K_AHEAD][t][e]), __uint_as_float(q[c][e]), x[t]);
+        } else {
+          x[t] = mma16<DT>(k[c % K_AHEAD][t], q[c], x[t]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (c + K_AHEAD < NQ) {
+        read_keys(c + K_AHEAD);
+      } else {                                            // (then what the softmax and the first product of values begin with)
+#pragma unroll
+        for (int i = 0; i < KT * 4; ++i)
+          if (i * K_AHEAD / (KT * 4) == c + K_AHEAD - NQ) add[i] = *reinterpret_cast<const float4*>(&added[8 * i + 4 * g]);
+        if (!FEW && c == NQ - 2) read_values(0);
+      }
+      if constexpr (!FEW) {                               // (the next block's loads while products go on)
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i * NQ / PER == c) load_one(Both(), i, next_keys, next_values);
+      }
+    }
+    if constexpr (!FEW) __builtin_amdgcn_s_setprio(0);
     if constexpr (FEW) {
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_wave_barrier();
@@ -420,18 +441,15 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
         next_block(s0 + step);
         load(Keys(), keys0, values0);
       }
-    } else {
-      read_values(0);
     }
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
-        const float4 add = *reinterpret_cast<const float4*>(&added[32 * t + 8 * r4 + 4 * g]);
-        x[t][4 * r4] = fmaf(x[t][4 * r4], a.scale, add.x);
-        x[t][4 * r4 + 1] = fmaf(x[t][4 * r4 + 1], a.scale, add.y);
-        x[t][4 * r4 + 2] = fmaf(x[t][4 * r4 + 2], a.scale, add.z);
-        x[t][4 * r4 + 3] = fmaf(x[t][4 * r4 + 3], a.scale, add.w);
+        x[t][4 * r4] = fmaf(x[t][4 * r4], scale, add[4 * t + r4].x);
+        x[t][4 * r4 + 1] = fmaf(x[t][4 * r4 + 1], scale, add[4 * t + r4].y);
+        x[t][4 * r4 + 2] = fmaf(x[t][4 * r4 + 2], scale, add[4 * t + r4].z);
+        x[t][4 * r4 + 3] = fmaf(x[t][4 * r4 + 3], scale, add[4 * t + r4].w);
       }
     if (CAUSAL && diagonal) {
 #pragma unroll
@@ -493,6 +511,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       }
     };
     weigh(0);
+    if constexpr (!FEW) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
       __builtin_amdgcn_sched_barrier(0);
@@ -511,6 +530,7 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
         __builtin_amdgcn_sched_group_barrier(0x402, DT == 0 ? 4 : (28 + M - 1) / M, 0);
       }
     }
+    if constexpr (!FEW) __builtin_amdgcn_s_setprio(0);
   };
   auto one = [&](int s0, char* keys, char* values, char* next_keys, char* next_values, float* added) STTM_INLINE {
     keys += set * NK * ROW;
@@ -628,9 +648,9 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       float add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
       for (int i = max(first, least - NK + 1); i < min(end, limit); ++i) {
-        const int page = PAGED ? table[i >> kk.pool.shift] : 0;
-        if ((PAGED && (unsigned)page >= (unsigned)kk.pool.pages) || (bias && bias[i] == -INFINITY)) continue;
-        const long long at = base + (PAGED ? page * kk.pool.page_stride + (i & kk.slot_mask) * stride : i * kk.token_stride);
+        const int page = PAGED ? table[i >> page_shift] : 0;
+        if ((PAGED && (unsigned)page >= (unsigned)pages) || (bias && bias[i] == -INFINITY)) continue;
+        const long long at = base + (PAGED ? page * page_stride + (i & slot_mask) * stride : i * kk.token_stride);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float v;
