@@ -116,6 +116,7 @@ inline float of_halves(float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); }
 inline void to_lds(const char* from, char* base) { memcpy(base + 16 * (threadIdx.x & 63), from, 16); }
 template <int LATER> inline void arrived() {}
 #define __builtin_amdgcn_sched_barrier(x) ((void)0)
+#define __builtin_amdgcn_s_setprio(x) ((void)0)
 #define __builtin_amdgcn_sched_group_barrier(kinds, count, group) ((void)0)
 #define __builtin_amdgcn_readlane(x, i) __shfl(x, i)
 #endif
