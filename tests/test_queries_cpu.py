@@ -1,6 +1,7 @@
 """The attention of several queries, its kernels compiled for host threads (tests/cpu_emul), against the definitions in 64 bits:
 indexing, masks, ragged sizes and refusals where there is no GPU."""
 import ctypes
+import os
 import shutil
 
 import pytest
@@ -15,7 +16,7 @@ def bench():
     from paper_2507_07990_amd import binding
     from tests.cpu_emul import build_cache_cpu
     real = binding._lib
-    binding._lib = binding._declare(ctypes.CDLL(build_cache_cpu.build()))
+    binding._lib = binding._declare(ctypes.CDLL(build_cache_cpu.build_sanitized() if "STTM_SANITIZED" in os.environ else build_cache_cpu.build()))
     try:
         ctx = binding.Sttm(0, stream_ptr=0)
         ctx._device_index = -1                  # (host tensors)
