@@ -351,8 +351,8 @@ size_t sttm_cache_evict_workspace_bytes(const sttm_cache* cache, const sttm_sequ
  * Queries. q, out [tokens, q_heads, d] (rows q_stride / out_stride elements apart, 16-byte aligned, the heads of a row one after the
  * other); q_heads is a multiple of kv_heads, head h reads key-value head h / (q_heads / kv_heads), q_heads / kv_heads <= 256. The tokens of
  * sequence b are the rows q_offsets[b] .. q_offsets[b + 1] - 1 (device int64 [batch + 1], ascending; NULL: one token for each sequence,
- * tokens == batch). Rows in front of the first sequence and behind the last one are neither read nor written. tokens <= 2^22, tokens *
- * q_heads / kv_heads <= 2^28. lse float [tokens, q_heads] (may be NULL) = log sum_j exp(s_j) over the keys that a query sees.
+ * tokens == batch). Rows in front of the first sequence and behind the last one are neither read nor written. out may be q with its stride;
+ * other overlaps are not allowed. tokens <= 2^22, tokens * q_heads / kv_heads <= 2^28. lse float [tokens, q_heads] (may be NULL) = log sum_j exp(s_j) over the keys that a query sees.
  * Scores and sums are held in fp32; a softmax weight is rounded to 16 bits before it meets a 16-bit value (fp16: as 2^15 times itself),
  * the result once more. A query with no key left gets out = 0, lse = -inf; a score that is NaN or +inf makes both NaN. An infinite value in a
  * slot that counts makes its channel infinite; infinities of both signs or a NaN make it NaN (and so may an infinite value whose weight is below
@@ -390,7 +390,7 @@ size_t sttm_cross_attention_workspace_bytes(const sttm_states* states, int64_t t
  * (block tables and lengths of the slots that a group shares); group g has the sequences group_offsets[g] .. group_offsets[g + 1] - 1
  * (device int32 [groups + 1], ascending; a sequence of no group has no prefix). prefixes NULL: none. seqs: each sequence's own slots, which
  * follow the prefix; the keys and values of its n tokens are its last n own slots already, and token j of them sees the prefix and the
- * own slots before length - (n - 1 - j). A prefix's keys and values are read once for all tokens of its group.
+ * own slots before length - (n - 1 - j). A prefix's keys and values are read from memory once for all tokens of its group.
  * prefix_bias float [groups, kv_heads, prefix_slots], key_bias float [batch, kv_heads, key_slots] (either may be NULL; entries from a
  * length on are not read): added to the scores, -inf masks a slot. As for sttm_paged_attention a page number outside the pool masks
  * its slots. Asynchronous. */

@@ -151,13 +151,12 @@ Plan make_plan(bool few, Cut a, Cut b, int64_t tokens, int q_heads, int d) {
   return p;
 }
 
-int check_queries(sttm_ctx* ctx, int64_t tokens, int batch, int q_heads, int kv_heads, int64_t max_len) {
+int check_queries(sttm_ctx* ctx, int64_t tokens, int q_heads, int kv_heads, int64_t max_len) {
   if (tokens < 0 || tokens > (1ll << 22)) return ctx_fail(ctx, STTM_ERR_SHAPE, "need 0 <= tokens <= 2^22");
   if (q_heads < 1 || q_heads % kv_heads || q_heads / kv_heads > 256 || q_heads > 65535)
     return ctx_fail(ctx, STTM_ERR_SHAPE, "need q_heads a multiple of kv_heads, at most 256 a kv head, q_heads <= 65535");
   if (tokens * (q_heads / kv_heads) > (1ll << 28)) return ctx_fail(ctx, STTM_ERR_SHAPE, "need tokens * q_heads / kv_heads <= 2^28");
   if ((double)tokens * q_heads * max_len > 1e15) return ctx_fail(ctx, STTM_ERR_SHAPE, "tokens * q_heads * keys too large");
-  (void)batch;
   return STTM_OK;
 }
 
@@ -223,6 +222,8 @@ template <int DT> void launch_all(QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs 
 }
 
 int launch(sttm_ctx* ctx, int dtype, QueryArgs a, KeyArgs ka, QueryArgs b, KeyArgs kb, const Plan& p, char* ws) {
+  const auto tiles = [&](const QueryArgs& x) { return x.tokens * x.group / query_tile(p.few) + x.segments; };
+  if ((tiles(a) * p.a.chunks + tiles(b) * p.b.chunks) * b.kv_heads >= 1ll << 32) return ctx_fail(ctx, STTM_ERR_SHAPE, "more than 2^32 pieces of work");
   const int rc = ctx_device(ctx);
   if (rc != STTM_OK) return rc;
   if (p.parts > 1) {
@@ -283,7 +284,7 @@ using namespace sttm;
 
 extern "C" size_t sttm_cross_attention_workspace_bytes(const sttm_states* states, int64_t tokens, int q_heads) {
   if (check_states(nullptr, states) != STTM_OK) return 0;
-  if (check_queries(nullptr, tokens, states->batch, q_heads, states->kv_heads, std::min<int64_t>(states->max_rows, states->rows)) != STTM_OK) return 0;
+  if (check_queries(nullptr, tokens, q_heads, states->kv_heads, std::min<int64_t>(states->max_rows, states->rows)) != STTM_OK) return 0;
   return plan_cross(states, tokens, q_heads).bytes;
 }
 
@@ -294,7 +295,7 @@ extern "C" int sttm_cross_attention(sttm_ctx* ctx, const sttm_states* states, in
   int rc = check_states(ctx, states);
   if (rc != STTM_OK) return rc;
   const int64_t max_len = std::min<int64_t>(states->max_rows, states->rows);
-  rc = check_queries(ctx, tokens, states->batch, q_heads, states->kv_heads, max_len);
+  rc = check_queries(ctx, tokens, q_heads, states->kv_heads, max_len);
   if (rc == STTM_OK) rc = check_rows(ctx, states->dtype, states->head_dim, q_heads, tokens, states->batch, q, q_stride, out, out_stride, q_offsets, scale);
   if (rc != STTM_OK) return rc;
   if (key_bias && bias_stride != 0 && (bias_stride < states->rows || bias_stride > (1ll << 40)))
@@ -326,7 +327,7 @@ extern "C" size_t sttm_shared_attention_workspace_bytes(const sttm_cache* cache,
       check_sequences(nullptr, cache, seqs) != STTM_OK)
     return 0;
   const int64_t max_len = (int64_t)make_seqs(cache, seqs).max_len + (prefixes ? make_seqs(cache, prefixes).max_len : 0);
-  if (check_queries(nullptr, tokens, seqs->batch, q_heads, cache->kv_heads, max_len) != STTM_OK) return 0;
+  if (check_queries(nullptr, tokens, q_heads, cache->kv_heads, max_len) != STTM_OK) return 0;
   return plan_shared(cache, prefixes, seqs, tokens, q_heads).bytes;
 }
 
@@ -340,7 +341,7 @@ extern "C" int sttm_shared_attention(sttm_ctx* ctx, const sttm_cache* cache, con
   if (rc == STTM_OK) rc = check_sequences(ctx, cache, seqs);
   if (rc != STTM_OK) return rc;
   const int64_t prefix_len = prefixes ? make_seqs(cache, prefixes).max_len : 0, own_len = make_seqs(cache, seqs).max_len, most = (int64_t)1 << 40;
-  rc = check_queries(ctx, tokens, seqs->batch, q_heads, cache->kv_heads, prefix_len + own_len);
+  rc = check_queries(ctx, tokens, q_heads, cache->kv_heads, prefix_len + own_len);
   if (rc == STTM_OK) rc = check_rows(ctx, cache->dtype, cache->head_dim, q_heads, tokens, seqs->batch, q, q_stride, out, out_stride, q_offsets, scale);
   if (rc != STTM_OK) return rc;
   if ((prefix_bias && (prefix_slots < prefix_len || prefix_slots > most)) || (key_bias && (key_slots < own_len || key_slots > most)))

@@ -321,6 +321,27 @@ def test_shared_attention_of_groups_with_offsets_that_make_no_sense(bench):
         assert out.shape == q.shape
 
 
+@pytest.mark.parametrize("dtype,tokens,n", [("bf16", 1, 70), ("f16", 40, 1100), ("f32", 2, 1100), ("f32", 70, 90)])
+def test_results_in_the_place_of_the_queries(bench, dtype, tokens, n):
+    """With one part a row and with several, few rows and many, against the call with a place of its own."""
+    gen, lib, page, d, H, K = _gen(n), bench.lib, 64, 32, 4, 2
+    storage, view = Q.states(gen, dtype, K, d, n, "projection")
+    kv, table = C.pool(gen, dtype, K, d, page, (n, tokens + 3))
+    q, q_offsets = torch.randn(tokens, H, d, generator=gen).to(TYPES[dtype]), bench.put(Q.offsets_of((tokens,)))
+    st = lib.States(*view([bench.put(x) for x in storage]), bench.put(Q.offsets_of((n,))))
+    cache, groups = lib.PagedCache(*[bench.put(x) for x in kv]), bench.put(torch.tensor([0, 1], dtype=torch.int32))
+    pre, own = (lib.Sequences(bench.put(table[i:i + 1]), bench.put(torch.tensor([m], dtype=torch.int32))) for i, m in enumerate((n, tokens + 3)))
+    ws = bench.workspace(max(lib.sttm_cross_attention_workspace_bytes(st, tokens, H), lib.sttm_shared_attention_workspace_bytes(cache, pre, own, tokens, H)))
+    calls = (lambda x, o: bench.ctx.sttm_cross_attention(x, st, o, 0.2, q_offsets=q_offsets, workspace=ws),
+             lambda x, o: bench.ctx.sttm_shared_attention(x, cache, pre, groups, own, o, 0.2, q_offsets=q_offsets, workspace=ws))
+    for call in calls:
+        apart, both = bench.guarded(torch.zeros_like(q)), bench.guarded(q)
+        call(bench.put(q), apart)
+        call(both, both)
+        bench.done()
+        assert torch.equal(apart, both)
+
+
 # -- refusals ----------------------------------------------------------------------------------------------------------
 
 def _refused(bench, code, call, *args, **kw):
