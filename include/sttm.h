@@ -357,7 +357,7 @@ size_t sttm_cache_evict_workspace_bytes(const sttm_cache* cache, const sttm_sequ
  * the result once more. A query with no key left gets out = 0, lse = -inf; a score that is NaN or +inf makes both NaN. An infinite value in a
  * slot that counts makes its channel infinite; infinities of both signs or a NaN make it NaN (and so may an infinite value whose weight is below
  * 2^-126 of the largest, fp16 2^-40, which counts as zero); what stands in a key or value that a query does not see does not matter. Values are
- * summed up before the division: |v| times the number of keys has to stay in fp32's range. Results do not depend on what else runs, nor on the order
+ * summed up before the division: |v| times the number of keys (bf16: 16 times as much) has to stay in fp32's range. Results do not depend on what else runs, nor on the order
  * of workgroups.
  * workspace: ..._workspace_bytes(...) bytes on the device, 256-byte aligned, overwritten at will; calls that overlap in time need
  * one each. */

@@ -197,6 +197,8 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
   constexpr int AT_ONCE = S::AT_ONCE, PER = S::PER, TILE = S::TILE;
   constexpr bool CAUSAL = PAGED;                          // (or may be)
   constexpr float LIFT = DT == 2 ? 15.f : 0.f;
+  // (as a weight up to 16, which costs sums that much of their range; fp16: 2^15.9, what it can hold; fp32 products take longer than the rescaling)
+  constexpr float SLACK = DT == 0 ? 0.f : DT == 1 ? 2.75f : 0.62f;
   constexpr float UNLIFT = DT == 2 ? 1.f / 32768.f : 1.f;
   constexpr int K_AHEAD = DT == 0 ? 2 : 4, V_AHEAD = 2;  // pieces of keys, steps of values read ahead
   constexpr bool ONE_WAY = DP * ES > 256;                 // (the registers that two ways take are not there)
@@ -465,9 +467,10 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[t][r]);
     top = of_halves(top);
-    const bool rises = __ballot(top > m) != 0;            // (seldom after the first blocks)
+    // What weights are relative to follows the maximum where that has risen by SLACK: of 32 rows one has a new maximum in most blocks.
+    const bool rises = __ballot(top > m + SLACK) != 0;
     const float before = m, from_before = m == -INFINITY ? -INFINITY : from;
-    m = fmaxf(m, top);
+    m = rises ? fmaxf(m, top) : m;
     from = m == -INFINITY ? 0.f : m * kLog2e;
     // Large scores: no multiple of theirs, only of their differences. (A rounding of `from` times 2^-24 is what an exponent may be off else.)
     float less = LIFT - from;
