@@ -204,8 +204,9 @@ __global__ void __launch_bounds__(kResidualThreads) k_residual_norm(ResidualArgs
 }
 
 // Rows follow one another in as many workgroups: twelve a compute unit, which holds three or four at once, so that they come out even (43,264
-// rows of 3,584 bf16 channels by 768 / 1,024 / 2,048 / 3,072 / one each: 235 / 292 / 246 / 237 / 280 us; 16,384 of 1,152 in fp32 75 / 67 / 68 / 69 / 78).
-constexpr int64_t kResidualBlocks = 3072;
+// rows of 3,584 bf16 channels by 3 / 4 / 8 / 10 / 11 / 12 / 14 a compute unit and one a row: 235 / 292 / 246 / 254 / 243 / 237 / 240 / 280 us; 16,384 of
+// 1,152 in fp32 75 / 67 / 68 / 71 / 68 / 69 / 69 / 78).
+constexpr int64_t kResidualBlocks = 12 * 256;
 
 template <int DT, int LANES, int U> void launch_rows(const ResidualArgs& a, bool once, hipStream_t s) {
   const int64_t blocks = (a.n + kResidualThreads / LANES - 1) / (kResidualThreads / LANES);
