@@ -475,7 +475,8 @@ __global__ void __launch_bounds__(query_waves(DT, DP, FEW) * kWave, query_waves_
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[t][r]);
     top = of_halves(top);
     // What weights are relative to follows the maximum where that has risen by SLACK: of 32 rows one has a new maximum in most blocks.
-    const bool rises = __ballot(top > m + SLACK) != 0;
+    // (The difference, not the sum: that one is rounded, to m + 1 where scores are 2^23. -inf less -inf is no rise.)
+    const bool rises = __ballot(top - m > SLACK) != 0;
     const float before = m, from_before = m == -INFINITY ? -INFINITY : from;
     m = rises ? fmaxf(m, top) : m;
     from = m == -INFINITY ? 0.f : m * kLog2e;

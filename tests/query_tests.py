@@ -133,6 +133,28 @@ def test_cross_attention_of_scores_near_the_largest_number(bench, dtype, heads, 
     close(got[1], torch.full((tokens, heads), big, dtype=torch.float64), 2.0 ** -22 * big, what="lse")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens", [1, 40])
+@pytest.mark.parametrize("apart", [1, 2, 4])
+def test_cross_attention_of_large_scores_that_rise_by_a_step(bench, dtype, tokens, apart):
+    """Scores of 2^23 and 2^23 + 1 (2^24 and 2^24 + 2, 2^25 and + 4): next to each other in 32 bits, the higher ones last."""
+    n = 400
+    storage, view = Q.states(_gen(n), dtype, 1, 8, n, "projection")
+    k, v = view(storage)
+    k[:], v[:, :, 0] = 0.0, 1.0
+    k[:, :, 0], k[300:, :, 1] = 4096.0, apart
+    q = torch.zeros(tokens, 2, 8)
+    q[:, :, 0], q[:, :, 1] = 2048.0 * apart, 1.0
+    got = Q.run_cross(bench, q.to(TYPES[dtype]), Q.offsets_of((tokens,)), storage, view, Q.offsets_of((n,)), 1.0)
+    # all products and sums up to here are exact: an even number of weights of 1 and of e^apart
+    w = torch.ones(n, dtype=torch.float64)
+    w[300:] = math.exp(apart)
+    w = w / w.sum()
+    want, size = w @ v[:, 0].double(), w @ v[:, 0].double().abs()
+    tol = size * ((n + 64) * C.E + (0 if dtype == "f32" else C.U[dtype])) + C.U[dtype] * 1.02 * want.abs() + (2.0 ** -40 * n * 8 if dtype == "f16" else 0)
+    close(got[0], want.expand(tokens, 2, 8), tol.expand(tokens, 2, 8), what="out")
+
+
 def test_cross_attention_of_large_products(bench):
     """Products of 3e38 at a scale of one, fp32."""
     n, tokens = 70, 4
