@@ -184,6 +184,52 @@ def test_residual_norm_of_many_rows(bench, dtype, n, D, gate):
     close(h[some.to(DEV)], *want[1], what="h")
 
 
+# -- the largest calls -------------------------------------------------------------------------------------------------
+
+def test_as_many_sequences_as_there_may_be(bench):
+    """65,535 sequences of one state, and of one own slot behind a prefix that none of them has: results are the values themselves."""
+    lib, n, d = bench.lib, 65535, 8
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    q, k, v = (torch.randn(n, 1, d, device=DEV, generator=gen).to(torch.bfloat16) for _ in range(3))
+    st = lib.States(k, v, torch.arange(n + 1, device=DEV), 1)
+    out, lse = torch.zeros_like(q), torch.zeros(n, 1, device=DEV)
+    bench.ctx.sttm_cross_attention(q, st, out, 0.5, lse=lse, workspace=bench.workspace(lib.sttm_cross_attention_workspace_bytes(st, n, 1)))
+    bench.done()
+    score = (q.double() * k.double()).sum(2) * 0.5
+    assert torch.equal(out, v) and float((lse.double() - score).abs().max()) < 1e-4
+    page, pages = 8, n // 8 + 1
+    pool = [torch.zeros(pages * page, d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    for x, y in zip(pool, (k, v)):
+        x[::page] = y[:pages, 0]
+    cache = lib.PagedCache(*[x.view(pages, 1, page, d) for x in pool])
+    own = lib.Sequences((torch.arange(n, device=DEV, dtype=torch.int32) % pages)[:, None].contiguous(), torch.ones(n, dtype=torch.int32, device=DEV), 1)
+    pre = lib.Sequences(torch.zeros(1, 1, dtype=torch.int32, device=DEV), torch.tensor([8], dtype=torch.int32, device=DEV), 8)
+    groups, out = torch.tensor([n, n], dtype=torch.int32, device=DEV), torch.zeros_like(q)
+    bench.ctx.sttm_shared_attention(q, cache, pre, groups, own, out, 0.5,
+                                    workspace=bench.workspace(lib.sttm_shared_attention_workspace_bytes(cache, pre, own, n, 1)))
+    bench.done()
+    assert torch.equal(out, v[torch.arange(n, device=DEV) % pages])
+
+
+def test_as_many_tokens_and_rows_as_there_may_be(bench):
+    lib, n, d = bench.lib, 1 << 22, 8
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    q = torch.randn(n, 1, d, device=DEV, generator=gen).to(torch.float16)
+    k, v = (torch.randn(300, 1, d, device=DEV, generator=gen).to(torch.float16) for _ in range(2))
+    st, out = lib.States(k, v, torch.tensor([0, 300], device=DEV)), torch.zeros_like(q)
+    bench.ctx.sttm_cross_attention(q, st, out, 0.3, q_offsets=torch.tensor([0, n], device=DEV),
+                                   workspace=bench.workspace(lib.sttm_cross_attention_workspace_bytes(st, n, 1)))
+    bench.done()
+    some = torch.cat([torch.arange(0, n, 9973, device=DEV), torch.arange(n - 200, n, device=DEV)])
+    want = _attend(q[some, 0], k[:, 0], v[:, 0], 0.3, None, None, "f16")
+    close(out[some, 0], want[0].cpu(), want[1].cpu(), what="out")
+    x = torch.randn(1 << 25, 8, device=DEV, generator=gen).to(torch.bfloat16)
+    r = torch.zeros_like(x)
+    bench.ctx.sttm_residual_norm(x, None, r, None, scale=2.0)
+    bench.done()
+    assert torch.equal(r, x * 2)
+
+
 # -- offsets beyond 32 bits --------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("tokens", [1, 70])
